@@ -713,6 +713,67 @@ int pyg_dense_transform_workspace(int64_t Fi, int64_t Fo, size_t *bytes);
 int pyg_dense_transform(const void *x, int x_dtype, int64_t N, int64_t Fi, const void *theta, int64_t Fo,
                         void *out, int out_dtype, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- Attention among the nodes of each graph of a mini-batch (Section 2,
+ * "Mini-batch Handling": the graphs of a batch follow one another), with a
+ * learned bias by relative position. GAT's attention (above) runs over edges;
+ * this one over all pairs of a graph's nodes. */
+
+/* One call's shapes and the bias (device pointers).
+ *   q_ptr   int64 [B+1], non-decreasing from 0: graph g's queries are rows q_ptr[g] ..
+ *           q_ptr[g+1]; k_ptr the same for keys and values (the same array where
+ *           every node is both). Rows from ptr[B] on belong to no graph.
+ *   H, Hkv  query heads and key/value heads; Hkv divides H, heads h of q read
+ *           head h / (H / Hkv) of k and v;  D <= 128 features a head.
+ *   *_row, *_head  strides of a row and of a head in elements; features are adjacent.
+ *   scale   factor c > 0 of the products.
+ *   causal  non-zero: key j is seen by query i only where j <= i + nk - nq (positions in
+ *           the graph; nk - nq aligns the last query with the last key).
+ *   table   [buckets, H] in dtype, or NULL (no bias): T[b, h];
+ *   bucket  int32 [2*reach+1]: the bucket of offset o - reach at place o (offsets
+ *           beyond the reach take its ends' buckets). Entries outside [0, buckets) are
+ *           read as the nearest one.
+ *   zero_rest  non-zero: rows of `out` of no graph get zeros, else they are left as they were. */
+typedef struct {
+    const int64_t *q_ptr, *k_ptr;
+    int64_t B, Nq, Nk, H, Hkv, D;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    int dtype;
+    float scale;
+    int causal;
+    const void *table;
+    const int32_t *bucket;
+    int64_t buckets, reach;
+    int zero_rest;
+} pyg_attention;
+
+/* Workspace bytes needed by pyg_global_attention (the pointers of *a are not read). */
+int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
+
+/* out[i, h] = sum_j p_ij v[j, h'], p_i = softmax over the keys j of i's graph of
+ * scale <q[i, h], k[j, h']> + T[bucket(j - (i + nk - nq)), h].
+ *   q [Nq, H, D], k and v [Nk, Hkv, D] with the strides of *a; out [Nq, H, D] contiguous;
+ *   stat  fp32 [Nq, H, 2] or NULL: what the backward needs of every row.
+ * A row that sees no key (none in its graph, all masked, all entries -infinity)
+ * gives zeros, and zero gradients. Scores, sums and statistics are fp32; bf16
+ * weights p are rounded to bf16 for the second product. Deterministic.
+ * Errors: PYG_ERR_INVALID_ARG (NULL or negative or inconsistent arguments,
+ * Hkv not dividing H, scale not in (0, 1e30], overlapping strides),
+ * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 4096, rows >= 2^31, a grid
+ * beyond 2^32 threads), PYG_ERR_WORKSPACE. */
+int pyg_global_attention(const pyg_attention *a, const void *q, const void *k, const void *v, void *out, float *stat,
+                         void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes needed by pyg_global_attention_backward. */
+int pyg_global_attention_backward_workspace(const pyg_attention *a, size_t *bytes);
+
+/* Gradients of the above from grad_out [Nq, H, D], the inputs, `out` and `stat` of the
+ * forward: grad_q [Nq, H, D], grad_k and grad_v [Nk, Hkv, D] (summed over the heads that
+ * share a key head in fp32), grad_table [buckets, H] or NULL, all contiguous, in dtype.
+ * Rows of no graph get zeros. Deterministic. Errors: as above. */
+int pyg_global_attention_backward(const pyg_attention *a, const void *grad_out, const void *q, const void *k,
+                                  const void *v, const void *out, const float *stat, void *grad_q, void *grad_k,
+                                  void *grad_v, void *grad_table, void *ws, size_t ws_bytes, void *stream);
+
 /* Workspace bytes needed by pyg_global_pool. */
 int pyg_global_pool_workspace(int dtype, int64_t N, int64_t F, int64_t B, int aggr, size_t *bytes);
 

@@ -61,3 +61,10 @@ from .binding import (  # noqa: F401
     validate_batch,
     validate_coo,
 )
+from .transformer import (  # noqa: F401
+    GlobalAttention,
+    global_attention,
+    global_attention_backward,
+    global_attention_workspace_bytes,
+    relative_buckets,
+)

@@ -36,6 +36,8 @@ EXPORTED = [
     "pyg_propagate_blocked", "pyg_gcn_propagate_blocked_workspace", "pyg_gcn_propagate_blocked",
     "pyg_coo_to_csr_blocked_workspace", "pyg_coo_to_csr_blocked", "pyg_degree_csr_blocks",
     "pyg_gat_forward_workspace", "pyg_gat_forward", "pyg_gat_backward_workspace", "pyg_gat_backward",
+    "pyg_global_attention_workspace", "pyg_global_attention", "pyg_global_attention_backward_workspace",
+    "pyg_global_attention_backward",
 ]
 
 
@@ -59,6 +61,15 @@ class _CsrBlocks(ctypes.Structure):
     _fields_ = [("rowptr", ctypes.c_void_p), ("col", ctypes.c_void_p), ("perm", ctypes.c_void_p),
                 ("weight", ctypes.c_void_p), ("N", ctypes.c_int64), ("E", ctypes.c_int64), ("B", ctypes.c_int64),
                 ("chunk", ctypes.c_int64)]
+
+
+class _Attention(ctypes.Structure):
+    _fields_ = [("q_ptr", ctypes.c_void_p), ("k_ptr", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int64) for n in ("B", "Nq", "Nk", "H", "Hkv", "D", "q_row", "q_head", "k_row", "k_head", "v_row",
+                                       "v_head")] + \
+        [("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("causal", ctypes.c_int), ("table", ctypes.c_void_p),
+         ("bucket", ctypes.c_void_p), ("buckets", ctypes.c_int64), ("reach", ctypes.c_int64),
+         ("zero_rest", ctypes.c_int)]
 
 
 _lib = None
@@ -143,6 +154,11 @@ def library() -> ctypes.CDLL:
             "pyg_dense_transform": [p, i32, i64, i64, p, i64, p, i32, p, ctypes.c_size_t, p],
             "pyg_global_pool_workspace": [i32, i64, i64, i64, i32, sz],
             "pyg_global_pool": [p, i32, i64, i64, p, i64, i32, p, p, p, ctypes.c_size_t, p],
+            "pyg_global_attention_workspace": [ctypes.POINTER(_Attention), sz],
+            "pyg_global_attention": [ctypes.POINTER(_Attention), p, p, p, p, p, p, ctypes.c_size_t, p],
+            "pyg_global_attention_backward_workspace": [ctypes.POINTER(_Attention), sz],
+            "pyg_global_attention_backward": [ctypes.POINTER(_Attention), p, p, p, p, p, p, p, p, p, p, p,
+                                              ctypes.c_size_t, p],
             "pyg_validate_coo": [p, i64, i64, p, p],
             "pyg_validate_batch": [p, i64, i64, p, p],
         }

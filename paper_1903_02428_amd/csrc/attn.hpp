@@ -1,0 +1,152 @@
+// What the attention kernels share: the call's arguments, the bias by relative
+// position, masks and the scores of a 32 x 32 tile.
+//
+// The scores are a_ij = c q_i . k_j + T[bucket(j - i'), h], with i' = i + nk - nq.
+// They are held as s = a / c: the bias over c is what a tile's accumulators
+// start from, so that the matrix cores add it and far from the diagonal, where
+// one bucket holds all offsets, it costs nothing. p = exp(a - max) is then
+// exp2(c2 (s - m)), c2 = c log2(e).
+#pragma once
+
+#include "attn_tiles.hpp"
+
+namespace pyg {
+namespace attn {
+
+struct Args {
+    const int64_t *q_ptr, *k_ptr;  // [B + 1]
+    int64_t B, Nq, Nk;
+    int H, Hkv, G, D;  // G = H / Hkv query heads share a key head
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;  // strides in elements
+    float scale, inv_scale, c2;
+    bool causal, vec_q, vec_k, vec_v, vec_o, zero_rest;
+    const void *table;    // [buckets, H] in the operands' type, or NULL
+    const int32_t *lut;   // [2 * reach + 1]
+    int buckets, reach;
+    const void *q, *k, *v;
+    void *out;
+    float *stat;  // [Nq, H, 2]: the row's largest s, log2 of its sum of exp2(c2 (s - m)); or NULL
+};
+
+constexpr int kMaxReach = 4096;
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__bf16 v) { return static_cast<float>(v); }
+
+// The bias over c of every offset, for head h, in LDS. Finite values stay
+// finite: a table entry of the type's lowest value masks without leaving the
+// row empty, as it does in the formula.
+template <typename T>
+__device__ __forceinline__ void stage_bias(const Args &a, int h, float *bias) {
+    const T *t = static_cast<const T *>(a.table);
+    for (int o = threadIdx.x; o <= 2 * a.reach; o += blockDim.x) {
+        float v = 0.f;
+        if (t) {
+            int b = a.lut[o];
+            b = b < 0 ? 0 : b >= a.buckets ? a.buckets - 1 : b;
+            const float raw = to_f32(t[(int64_t)b * a.H + h]);
+            v = raw * a.inv_scale;
+            if (fabsf(raw) <= -kLowest) v = fminf(fmaxf(v, kLowest), -kLowest);
+        }
+        bias[o] = v;
+    }
+}
+
+// The other half's value of the same column (lanes l and l ^ 32).
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// Start of a 32 x 32 tile of scores whose lane holds column offset `col` and
+// rows 8 (r / 4) + 4 h + r % 4, offsets (key minus query) d0 + SIGN-ed index:
+// KEYS_IN_ROWS: rows are keys, the lane's column a query: d = d0 + row - m;
+// else rows are queries and the column a key: d = d0 + m - row.
+template <bool KEYS_IN_ROWS>
+__device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int64_t d0, int lane) {
+    f32x16 c;
+    // offsets of the tile: d0 - 31 .. d0 + 31
+    if (d0 - 31 >= reach || d0 + 31 <= -reach) {
+        const float v = bias[d0 > 0 ? 2 * reach : 0];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) c[r] = v;
+        return c;
+    }
+    const int m = lane & 31, h = lane >> 5, base = static_cast<int>(d0) + reach;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int row = 8 * (r >> 2) + 4 * h + (r & 3);
+        int o = base + (KEYS_IN_ROWS ? row - m : m - row);
+        o = o < 0 ? 0 : o > 2 * reach ? 2 * reach : o;
+        c[r] = bias[o];
+    }
+    return c;
+}
+
+// -infinity where there is no such key (rows from `keys` on) or it comes later
+// than the query (causal, offset > 0).
+template <bool KEYS_IN_ROWS>
+__device__ __forceinline__ void mask_tile(f32x16 &c, int64_t keys, int64_t queries, bool causal, int64_t d0, int lane) {
+    if (keys >= 32 && queries >= 32 && (!causal || d0 + 31 <= 0)) return;
+    const int m = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int row = 8 * (r >> 2) + 4 * h + (r & 3);
+        const int key = KEYS_IN_ROWS ? row : m, query = KEYS_IN_ROWS ? m : row;
+        if (key >= keys || query >= queries || (causal && d0 + key - query > 0)) c[r] = kNegInf;
+    }
+}
+
+// From this size on, c2 s - c2 m in one fused multiply-add leaves more than the
+// exponent's own rounding (a table of lowest values): s - m comes first there.
+constexpr float kWild = 65536.f;
+
+// Rows [first, last) of a [N, H, D] output, head h, get zeros (rows of no graph).
+template <typename T>
+__device__ __forceinline__ void zero_rows(T *out, int64_t first, int64_t last, int H, int h, int D) {
+    const int64_t n = (last - first) * D;
+    for (int64_t i = threadIdx.x; i < n; i += blockDim.x) {
+        const int64_t row = first + i / D;
+        out[(row * H + h) * D + i % D] = T(0.f);
+    }
+}
+
+// out[row, head h] from a wavefront's D x 32 result (lane: column = row, registers = features), times `mul`.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(T *out, int64_t row, bool there, int H, int h, int D, bool vec,
+                                           const f32x16 (&acc)[DP / 32], float mul, int lane) {
+    if (!there) return;
+    T *o = out + (row * H + h) * D;
+    const int hh = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 32 * t + 8 * r + 4 * hh;
+            if (d >= D) continue;
+            const float v0 = acc[t][4 * r] * mul, v1 = acc[t][4 * r + 1] * mul, v2 = acc[t][4 * r + 2] * mul,
+                        v3 = acc[t][4 * r + 3] * mul;
+            if (vec) {
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(o + d) = make_uint2(pack_bf16(v0, v1), pack_bf16(v2, v3));
+                else *reinterpret_cast<float4 *>(o + d) = make_float4(v0, v1, v2, v3);
+            } else {
+                const float v[4] = {v0, v1, v2, v3};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (d + i < D) o[d + i] = T(v[i]);
+            }
+        }
+}
+
+int forward(const Args &a, bool bf16, hipStream_t s);
+// The same where a graph has few queries: its keys cut into few_splits() ranges.
+int few_splits(const Args &a);
+int forward_few(const Args &a, bool bf16, void *ws, hipStream_t s);
+
+struct BackwardArgs {
+    Args f;  // out: the forward's result
+    const void *grad_out;
+    void *grad_q, *grad_k, *grad_v, *grad_table;  // each or NULL (grad_table)
+};
+size_t backward_workspace(const Args &a);
+int backward(const BackwardArgs &a, bool bf16, void *ws, hipStream_t s);
+
+}  // namespace attn
+}  // namespace pyg

@@ -1,0 +1,278 @@
+// Attention among the nodes of each graph of a batch with a learned bias by
+// relative position: forward.
+#include "attn.hpp"
+
+namespace pyg {
+namespace attn {
+namespace {
+
+// A workgroup owns 32 * WAVES queries of one graph and head and walks over the
+// graph's keys in tiles of BK, staged in LDS for its wavefronts; a wavefront
+// keeps 32 queries. S^T = K Q^T puts a query in a lane's column, so the running
+// maximum and sum are one value a lane and P^T is the second product's operand
+// as it stands: O^T = V^T P^T.
+template <typename T, int DP, int WAVES, int BK>
+__global__ __launch_bounds__(64 * WAVES) void k_forward(const Args a, int64_t nslots) {
+    constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
+    constexpr int stride = tile_stride<T, DP>();
+    extern __shared__ __align__(16) char lds[];
+    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BK * stride;
+    float *bias = reinterpret_cast<float *>(vt + BK * stride);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    // key heads vary fastest: with up to 8 of them (or a multiple) every XCD's L2 sees its own heads' keys only
+    const int64_t id = blockIdx.x;
+    const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
+    const int64_t slot = nslots - 1 - id / a.H;  // causal: the longest walks first
+    const Place pq = place_of(a.q_ptr, a.B, a.Nq, slot, BM, 1, lane);
+    const int64_t q0 = pq.first + pq.tile * BM;  // the workgroup's first query row
+    if (pq.tile < 0 || q0 >= pq.last) return;
+    T *out = static_cast<T *>(a.out);
+    if (pq.graph == a.B) {
+        if (a.zero_rest) zero_rows(out, q0, q0 + BM < pq.last ? q0 + BM : pq.last, a.H, head, a.D);
+        return;
+    }
+    stage_bias<T>(a, head, bias);
+    const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
+                  k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
+    const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
+    const T *kb = static_cast<const T *>(a.k) + hk * a.k_head, *vb = static_cast<const T *>(a.v) + hk * a.v_head;
+
+    const int64_t i0 = pq.tile * BM + wave * 32;           // first query of the wavefront, in the graph
+    const int64_t row = pq.first + i0 + m;                 // the lane's query row
+    const bool there = row < pq.last;
+    uint4 qf[SQ];
+    const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < SQ; ++s) qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, a.vec_q, there);
+
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) acc[t] = f32x16(0.f);
+    float top = kNegInf, sum = 0.f;  // of the lane's query: sum over this half's keys
+
+    int64_t end = nk;
+    if (a.causal) {
+        const int64_t seen = pq.tile * BM + BM + nk - nq;  // keys that the last query of the workgroup may see
+        end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
+    }
+    Stage<T, DP, BK, NT> sk, sv;
+    if (end > 0) {
+        sk.load(kb, a.k_row, k_first, k_last, a.D, a.vec_k);
+        sv.load(vb, a.v_row, k_first, k_last, a.D, a.vec_v);
+    }
+    for (int64_t j0 = 0; j0 < end; j0 += BK) {
+        __syncthreads();
+        sk.store(kt);
+        sv.store(vt);
+        __syncthreads();
+        if (j0 + BK < end) {
+            sk.load(kb, a.k_row, k_first + j0 + BK, k_last, a.D, a.vec_k);
+            sv.load(vb, a.v_row, k_first + j0 + BK, k_last, a.D, a.vec_v);
+        }
+        const int64_t d0 = j0 - (i0 + nk - nq);  // offset of the tile's first key and the wavefront's first query
+        if (a.causal && d0 > 31) continue;       // later than all of the wavefront's queries
+        f32x16 st[NK];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            st[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
+#pragma unroll
+            for (int s = 0; s < SQ; ++s) st[n] = mma<T>(row_piece<T, DP>(kt, 32 * n + m, s, h), qf[s], st[n]);
+            mask_tile<true>(st[n], nk - j0 - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+        }
+        float t = kNegInf;
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) t = fmaxf(t, st[n][r]);
+        t = fmaxf(t, other_half(t));
+        const float top_new = fmaxf(top, t), ref = top_new == kNegInf ? 0.f : top_new;
+        const float shrink = __builtin_amdgcn_exp2f(a.c2 * (top - ref));
+        top = top_new;
+        sum *= shrink;
+        if (__any(shrink != 1.f)) {
+#pragma unroll
+            for (int u = 0; u < DP / 32; ++u) acc[u] *= shrink;
+        }
+        if (__any(fabsf(ref) > kWild)) {
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[n][r] = __builtin_amdgcn_exp2f(a.c2 * (st[n][r] - ref));
+        } else {
+            const float z = -a.c2 * ref;
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, st[n][r], z));
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += st[n][r];
+#pragma unroll
+            for (int u = 0; u < Elem<T>::kSteps; ++u) {
+                // P is rounded to the operands' type for the matrix cores: at most half a step of that type on each
+                // summand, no more than the result's own rounding; the sum of P keeps 32 bits
+                const uint4 p = piece_of<T>(st[n], u);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) acc[d] = mma<T>(col_piece<T, DP>(vt, 32 * n, 32 * d, u, lane), p, acc[d]);
+            }
+        }
+    }
+    sum += other_half(sum);
+    store_rows<T, DP>(out, row, there, a.H, head, a.D, a.vec_o, acc, top == kNegInf ? 0.f : 1.f / sum, lane);
+    if (a.stat && there && h == 0)
+        *reinterpret_cast<float2 *>(a.stat + (row * a.H + head) * 2) = make_float2(top, top == kNegInf ? 0.f : __log2f(sum));
+}
+
+template <typename T, int DP, int WAVES, int BK>
+int launch(const Args &a, hipStream_t s) {
+    const int64_t n = slots(a.Nq, a.B, 32 * WAVES);
+    const size_t bytes = 2 * BK * tile_stride<T, DP>() * sizeof(T) + (2 * a.reach + 1) * sizeof(float);
+    if (n * a.H >= (int64_t(1) << 32) / (64 * WAVES)) return PYG_ERR_UNSUPPORTED;
+    k_forward<T, DP, WAVES, BK><<<static_cast<unsigned>(n * a.H), 64 * WAVES, bytes, s>>>(a, n);
+    PYG_LAUNCH_CHECK();
+    return PYG_OK;
+}
+
+template <typename T, int DP>
+int by_waves(const Args &a, hipStream_t s) {
+    if (a.Nq <= 64 * a.B) return launch<T, DP, 1, 32>(a, s);
+    return launch<T, DP, 4, 64>(a, s);
+}
+
+template <typename T>
+int by_width(const Args &a, hipStream_t s) {
+    if (a.D <= 32) return by_waves<T, 32>(a, s);
+    if (a.D <= 64) return by_waves<T, 64>(a, s);
+    return by_waves<T, 128>(a, s);
+}
+
+}  // namespace
+
+int forward(const Args &a, bool bf16, hipStream_t s) { return bf16 ? by_width<__bf16>(a, s) : by_width<float>(a, s); }
+
+}  // namespace attn
+
+namespace {
+
+using namespace attn;
+
+constexpr int64_t kMax32 = int64_t(1) << 31;
+
+// Query rows that share a key head, on average over the graphs, up to which
+// the 16-row form takes them.
+bool few(const Args &a) { return a.Nq * a.G <= 16 * a.B; }
+
+bool vectors(const void *p, int64_t row, int64_t head, int64_t D, size_t e) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && row * e % 16 == 0 && head * e % 16 == 0 && D * e % 16 == 0;
+}
+
+// Host checks of a call; fills the kernels' arguments.
+int take(const pyg_attention *c, Args *a) {
+    if (!c) return PYG_ERR_INVALID_ARG;
+    if (c->dtype != PYG_F32 && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
+    if (c->B < 0 || c->Nq < 0 || c->Nk < 0 || c->H < 1 || c->Hkv < 1 || c->D < 1 || c->H % c->Hkv) return PYG_ERR_INVALID_ARG;
+    if (!(c->scale > 0.f) || c->scale > 1e30f) return PYG_ERR_INVALID_ARG;
+    if (c->Nq >= kMax32 || c->Nk >= kMax32 || c->B >= kMax32 || c->D > 128 || c->H > 65535) return PYG_ERR_UNSUPPORTED;
+    if (c->table) {
+        if (!c->bucket || c->buckets < 1 || c->reach < 0) return PYG_ERR_INVALID_ARG;
+        if (c->reach > kMaxReach || c->buckets > kMaxReach) return PYG_ERR_UNSUPPORTED;
+    }
+    *a = Args{};
+    a->q_ptr = c->q_ptr, a->k_ptr = c->k_ptr;
+    a->B = c->B, a->Nq = c->Nq, a->Nk = c->Nk;
+    a->H = static_cast<int>(c->H), a->Hkv = static_cast<int>(c->Hkv), a->G = a->H / a->Hkv, a->D = static_cast<int>(c->D);
+    a->q_row = c->q_row, a->q_head = c->q_head, a->k_row = c->k_row, a->k_head = c->k_head, a->v_row = c->v_row,
+    a->v_head = c->v_head;
+    a->scale = c->scale, a->inv_scale = 1.f / c->scale, a->c2 = c->scale * 1.4426950408889634f;
+    a->causal = c->causal != 0, a->zero_rest = c->zero_rest != 0;
+    a->table = c->table, a->lut = c->table ? c->bucket : nullptr;
+    a->buckets = c->table ? static_cast<int>(c->buckets) : 0, a->reach = c->table ? static_cast<int>(c->reach) : 0;
+    return PYG_OK;
+}
+
+size_t bytes_of(const pyg_attention *c) { return c->dtype == PYG_BF16 ? 2 : 4; }
+
+// Whether N rows of H heads of D features do not overlap: heads inside rows, or rows inside heads.
+bool strided(int64_t row, int64_t head, int64_t N, int64_t H, int64_t D) {
+    if ((N > 1 && row < D) || (H > 1 && head < D)) return false;
+    return N <= 1 || H <= 1 || row >= head * (H - 1) + D || head >= row * (N - 1) + D;
+}
+
+int take_inputs(const pyg_attention *c, const void *q, const void *k, const void *v, Args *a) {
+    if (!c->q_ptr || !c->k_ptr) return PYG_ERR_INVALID_ARG;
+    if ((c->Nq > 0 && !q) || (c->Nk > 0 && (!k || !v))) return PYG_ERR_INVALID_ARG;
+    if (!strided(c->q_row, c->q_head, c->Nq, c->H, c->D) || !strided(c->k_row, c->k_head, c->Nk, c->Hkv, c->D) ||
+        !strided(c->v_row, c->v_head, c->Nk, c->Hkv, c->D))
+        return PYG_ERR_INVALID_ARG;
+    const size_t e = bytes_of(c);
+    a->q = q, a->k = k, a->v = v;
+    a->vec_q = vectors(q, c->q_row, c->q_head, c->D, e);
+    a->vec_k = vectors(k, c->k_row, c->k_head, c->D, e);
+    a->vec_v = vectors(v, c->v_row, c->v_head, c->D, e);
+    return PYG_OK;
+}
+
+}  // namespace
+}  // namespace pyg
+
+using namespace pyg;
+
+extern "C" int pyg_global_attention_workspace(const pyg_attention *c, size_t *bytes) {
+    Args a;
+    if (!bytes) return PYG_ERR_INVALID_ARG;
+    PYG_TRY(take(c, &a));
+    *bytes = 0;
+    if (a.B > 0 && few(a)) {
+        const int s = few_splits(a);
+        if (s > 1) *bytes = static_cast<size_t>(a.Nq) * a.H * s * (a.D + 2) * sizeof(float);
+    }
+    return PYG_OK;
+}
+
+extern "C" int pyg_global_attention(const pyg_attention *c, const void *q, const void *k, const void *v, void *out,
+                                    float *stat, void *ws, size_t ws_bytes, void *stream) {
+    Args a;
+    size_t need = 0;
+    PYG_TRY(take(c, &a));
+    PYG_TRY(take_inputs(c, q, k, v, &a));
+    if (a.Nq > 0 && !out) return PYG_ERR_INVALID_ARG;
+    PYG_TRY(pyg_global_attention_workspace(c, &need));
+    if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
+    if (a.Nq == 0) return PYG_OK;
+    a.out = out, a.stat = stat;
+    a.vec_o = vectors(out, a.D, a.D, a.D, bytes_of(c));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool bf16 = c->dtype == PYG_BF16;
+    return a.B > 0 && few(a) ? attn::forward_few(a, bf16, ws, s) : attn::forward(a, bf16, s);
+}
+
+extern "C" int pyg_global_attention_backward_workspace(const pyg_attention *c, size_t *bytes) {
+    Args a;
+    if (!bytes) return PYG_ERR_INVALID_ARG;
+    PYG_TRY(take(c, &a));
+    *bytes = attn::backward_workspace(a);
+    return PYG_OK;
+}
+
+extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void *grad_out, const void *q, const void *k,
+                                             const void *v, const void *out, const float *stat, void *grad_q, void *grad_k,
+                                             void *grad_v, void *grad_table, void *ws, size_t ws_bytes, void *stream) {
+    attn::BackwardArgs b{};
+    PYG_TRY(take(c, &b.f));
+    PYG_TRY(take_inputs(c, q, k, v, &b.f));
+    Args &a = b.f;
+    if (a.Nq > 0 && (!grad_out || !out || !stat || !grad_q)) return PYG_ERR_INVALID_ARG;
+    if (a.Nk > 0 && (!grad_k || !grad_v)) return PYG_ERR_INVALID_ARG;
+    if (grad_table && !c->table) return PYG_ERR_INVALID_ARG;
+    const size_t need = attn::backward_workspace(a);
+    if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
+    a.out = const_cast<void *>(out), a.stat = const_cast<float *>(stat);
+    b.grad_out = grad_out, b.grad_q = grad_q, b.grad_k = grad_k, b.grad_v = grad_v, b.grad_table = grad_table;
+    a.vec_o = true;
+    for (const void *p : {grad_out, out, static_cast<const void *>(grad_q), static_cast<const void *>(grad_k),
+                          static_cast<const void *>(grad_v)})
+        a.vec_o = a.vec_o && vectors(p, a.D, a.D, a.D, bytes_of(c));
+    return attn::backward(b, c->dtype == PYG_BF16, ws, static_cast<hipStream_t>(stream));
+}

@@ -1,0 +1,379 @@
+// Attention among the nodes of each graph of a batch with a learned bias by
+// relative position: gradients. With P the softmax's rows and g the gradient of
+// the output,
+//   delta_i = sum_d g_id o_id,  dP = g V^T,  dS = P (dP - delta),
+//   dQ = c dS K,  dK = c dS^T Q,  dV = P^T g,  dT[b, h] = sum of dS over bucket b.
+// P and dS are made again from the row statistics that the forward kept, once
+// by the kernel that owns queries (dQ, delta, dT) and once by the one that owns
+// keys (dK, dV): no gradient is added to by two workgroups, so the results do
+// not depend on their order.
+#include "attn.hpp"
+
+namespace pyg {
+namespace attn {
+namespace {
+
+// exp2 of a score tile's registers, normalised: exp2(c2 (s - top) - log2 sum).
+struct RowStat {
+    float top, log_sum, lse;  // lse = c2 top + log2 sum, infinite for a row that sees no key
+};
+__device__ __forceinline__ RowStat row_stat(const float *__restrict__ stat, int64_t at, float c2) {
+    const float2 s = *reinterpret_cast<const float2 *>(stat + 2 * at);
+    return {s.x, s.y, s.x == kNegInf ? -kNegInf : fmaf(c2, s.x, s.y)};
+}
+constexpr RowStat kNoRow{kNegInf, 0.f, -kNegInf};
+
+// A workgroup owns 32 * WAVES queries, as in the forward.
+template <typename T, int DP, int WAVES, int BK>
+__global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int64_t nslots, float *__restrict__ delta,
+                                                       float *__restrict__ part) {
+    const Args &a = b.f;
+    constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
+    constexpr int stride = tile_stride<T, DP>();
+    extern __shared__ __align__(16) char lds[];
+    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BK * stride;
+    float *bias = reinterpret_cast<float *>(vt + BK * stride);
+    float *hist = bias + (2 * a.reach + 1);  // a wavefront's own sums by offset
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int64_t id = blockIdx.x;
+    const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
+    const int64_t slot = nslots - 1 - id / a.H;
+    float *mine = part ? part + (slot * a.H + head) * a.buckets : nullptr;  // the workgroup's share of dT
+    const Place pq = place_of(a.q_ptr, a.B, a.Nq, slot, BM, 1, lane);
+    const int64_t q0 = pq.first + pq.tile * BM;
+    if (pq.tile < 0 || q0 >= pq.last || pq.graph == a.B) {
+        if (mine)
+            for (int i = threadIdx.x; i < a.buckets; i += NT) mine[i] = 0.f;
+        if (pq.graph == a.B && pq.tile >= 0 && q0 < pq.last)
+            zero_rows(static_cast<T *>(b.grad_q), q0, q0 + BM < pq.last ? q0 + BM : pq.last, a.H, head, a.D);
+        return;
+    }
+    const int offsets = 2 * a.reach + 1;
+    stage_bias<T>(a, head, bias);
+    if (mine)
+        for (int i = threadIdx.x; i < offsets * WAVES; i += NT) hist[i] = 0.f;
+    float *own = hist + wave * offsets;
+    const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
+                  k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
+    const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
+    const T *kb = static_cast<const T *>(a.k) + hk * a.k_head, *vb = static_cast<const T *>(a.v) + hk * a.v_head;
+
+    const int64_t i0 = pq.tile * BM + wave * 32, row = pq.first + i0 + m;
+    const bool there = row < pq.last;
+    uint4 qf[SQ], gf[SQ];
+    const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
+    const T *gr = static_cast<const T *>(b.grad_out) + (row * a.H + head) * a.D;
+    const T *orow = static_cast<const T *>(a.out) + (row * a.H + head) * a.D;
+    float dl = 0.f;
+#pragma unroll
+    for (int s = 0; s < SQ; ++s) {
+        qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, a.vec_q, there);
+        Piece<T> g, o;
+        g.u = gf[s] = load_piece<T>(gr, 2 * E * s + E * h, a.D, a.vec_o, there);
+        o.u = load_piece<T>(orow, 2 * E * s + E * h, a.D, a.vec_o, there);
+#pragma unroll
+        for (int i = 0; i < E; ++i) dl = fmaf(to_f32(g.v[i]), to_f32(o.v[i]), dl);
+    }
+    dl += other_half(dl);
+    RowStat st = kNoRow;
+    if (there) {
+        st = row_stat(a.stat, row * a.H + head, a.c2);
+        if (h == 0) delta[row * a.H + head] = dl;
+    }
+    const bool wild = __any(st.top != kNegInf && fabsf(st.top) > kWild);
+
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) acc[t] = f32x16(0.f);
+    float below = 0.f, above = 0.f;  // the lane's dS of whole tiles beyond the reach
+
+    int64_t end = nk;
+    if (a.causal) {
+        const int64_t seen = pq.tile * BM + BM + nk - nq;
+        end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
+    }
+    Stage<T, DP, BK, NT> sk, sv;
+    if (end > 0) {
+        sk.load(kb, a.k_row, k_first, k_last, a.D, a.vec_k);
+        sv.load(vb, a.v_row, k_first, k_last, a.D, a.vec_v);
+    }
+    for (int64_t j0 = 0; j0 < end; j0 += BK) {
+        __syncthreads();
+        sk.store(kt);
+        sv.store(vt);
+        __syncthreads();
+        if (j0 + BK < end) {
+            sk.load(kb, a.k_row, k_first + j0 + BK, k_last, a.D, a.vec_k);
+            sv.load(vb, a.v_row, k_first + j0 + BK, k_last, a.D, a.vec_v);
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            const int64_t d0 = j0 + 32 * n - (i0 + nk - nq);
+            if ((a.causal && d0 > 31) || j0 + 32 * n >= nk) continue;
+            f32x16 s = bias_tile<true>(bias, a.reach, d0, lane), dp = f32x16(0.f);
+#pragma unroll
+            for (int u = 0; u < SQ; ++u) {
+                s = mma<T>(row_piece<T, DP>(kt, 32 * n + m, u, h), qf[u], s);
+                dp = mma<T>(row_piece<T, DP>(vt, 32 * n + m, u, h), gf[u], dp);
+            }
+            mask_tile<true>(s, nk - j0 - 32 * n, 32, a.causal, d0, lane);
+            if (wild) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[r] = st.top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(a.c2, s[r] - st.top, -st.log_sum));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[r], -st.lse));
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] *= dp[r] - dl;  // dS^T
+            if (mine) {
+                if (d0 - 31 >= a.reach || d0 + 31 <= -a.reach) {
+                    float t = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) t += s[r];
+                    (d0 > 0 ? above : below) += t;
+                } else {
+                    // at most two lanes of an instruction meet in an offset: their column and row differ alike
+                    const int base = static_cast<int>(d0) + a.reach - m + 4 * h;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        int o = base + 8 * (r >> 2) + (r & 3);
+                        o = o < 0 ? 0 : o >= offsets ? offsets - 1 : o;
+                        atomicAdd(own + o, s[r]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < Elem<T>::kSteps; ++u) {
+                const uint4 p = piece_of<T>(s, u);  // dS rounded once to the operands' type
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) acc[t] = mma<T>(col_piece<T, DP>(kt, 32 * n, 32 * t, u, lane), p, acc[t]);
+            }
+        }
+    }
+    store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
+    if (mine) {
+        for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o), above += __shfl_xor(above, o);
+        if (lane == 0) own[0] += below, own[offsets - 1] += above;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.buckets; i += NT) {
+            float t = 0.f;
+            for (int o = 0; o < offsets; ++o) {
+                int l = a.lut[o];
+                l = l < 0 ? 0 : l >= a.buckets ? a.buckets - 1 : l;
+                if (l != i) continue;
+                for (int w = 0; w < WAVES; ++w) t += hist[w * offsets + o];
+            }
+            mine[i] = t;
+        }
+    }
+}
+
+// A workgroup owns 32 * WAVES keys of one graph and key head and walks over
+// the queries of all G heads that share it, in tiles of BQ. S = Q K^T puts a
+// key in a lane's column: P and dS are the operands of dV^T = g^T P and
+// dK^T = Q^T dS as they stand.
+template <typename T, int DP, int WAVES, int BQ>
+__global__ __launch_bounds__(64 * WAVES) void k_grad_kv(const BackwardArgs b, int64_t nslots,
+                                                        const float *__restrict__ delta) {
+    const Args &a = b.f;
+    constexpr int NT = 64 * WAVES, BN = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NQ = BQ / 32;
+    constexpr int stride = tile_stride<T, DP>();
+    extern __shared__ __align__(16) char lds[];
+    T *qt = reinterpret_cast<T *>(lds), *gt = qt + BQ * stride;
+    float *stats = reinterpret_cast<float *>(gt + BQ * stride);  // [BQ] each: lse, top, delta, log2 sum
+    float *bias = stats + 4 * BQ;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int64_t id = blockIdx.x;
+    const int hk = id % a.Hkv;
+    const int64_t slot = id / a.Hkv;  // causal: the first keys are seen by the most queries
+    const Place pk = place_of(a.k_ptr, a.B, a.Nk, slot, BN, 1, lane);
+    const int64_t k0 = pk.first + pk.tile * BN;
+    if (pk.tile < 0 || k0 >= pk.last) return;
+    if (pk.graph == a.B) {
+        const int64_t e = k0 + BN < pk.last ? k0 + BN : pk.last;
+        zero_rows(static_cast<T *>(b.grad_k), k0, e, a.Hkv, hk, a.D);
+        zero_rows(static_cast<T *>(b.grad_v), k0, e, a.Hkv, hk, a.D);
+        return;
+    }
+    const int64_t q_first = uniform64(ptr_at(a.q_ptr, pk.graph, a.Nq)),
+                  q_last = uniform64(ptr_at(a.q_ptr, pk.graph + 1, a.Nq));
+    const int64_t nq = q_last > q_first ? q_last - q_first : 0, nk = pk.last - pk.first;
+    const int64_t j0 = pk.tile * BN + wave * 32, row = pk.first + j0 + m;
+    const bool there = row < pk.last;
+    uint4 kf[SQ], vf[SQ];
+    const T *kr = static_cast<const T *>(a.k) + row * a.k_row + hk * a.k_head;
+    const T *vr = static_cast<const T *>(a.v) + row * a.v_row + hk * a.v_head;
+#pragma unroll
+    for (int s = 0; s < SQ; ++s) {
+        kf[s] = load_piece<T>(kr, 2 * E * s + E * h, a.D, a.vec_k, there);
+        vf[s] = load_piece<T>(vr, 2 * E * s + E * h, a.D, a.vec_v, there);
+    }
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = f32x16(0.f);
+
+    int64_t begin = 0;
+    if (a.causal) {  // the first query that sees the workgroup's first key
+        begin = pk.tile * BN - (nk - nq);
+        begin = begin < 0 ? 0 : begin / 32 * 32;
+    }
+    for (int g = 0; g < a.G; ++g) {
+        const int head = hk * a.G + g;
+        __syncthreads();
+        stage_bias<T>(a, head, bias);
+        const T *qb = static_cast<const T *>(a.q) + head * a.q_head;
+        const T *gb = static_cast<const T *>(b.grad_out) + (int64_t)head * a.D;
+        const int64_t g_row = (int64_t)a.H * a.D;
+        Stage<T, DP, BQ, NT> sq, sg;
+        if (begin < nq) {
+            sq.load(qb, a.q_row, q_first + begin, q_last, a.D, a.vec_q);
+            sg.load(gb, g_row, q_first + begin, q_last, a.D, a.vec_o);
+        }
+        for (int64_t i0 = begin; i0 < nq; i0 += BQ) {
+            __syncthreads();
+            sq.store(qt);
+            sg.store(gt);
+            for (int i = threadIdx.x; i < BQ; i += NT) {
+                const int64_t r = q_first + i0 + i;
+                RowStat st = kNoRow;
+                float dl = 0.f;
+                if (r < q_last) {
+                    st = row_stat(a.stat, r * a.H + head, a.c2);
+                    dl = delta[r * a.H + head];
+                }
+                stats[i] = st.lse, stats[BQ + i] = st.top, stats[2 * BQ + i] = dl, stats[3 * BQ + i] = st.log_sum;
+            }
+            __syncthreads();
+            if (i0 + BQ < nq) {
+                sq.load(qb, a.q_row, q_first + i0 + BQ, q_last, a.D, a.vec_q);
+                sg.load(gb, g_row, q_first + i0 + BQ, q_last, a.D, a.vec_o);
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const int64_t d0 = j0 - (i0 + 32 * n + nk - nq);
+                if ((a.causal && d0 > 31) || i0 + 32 * n >= nq) continue;
+                f32x16 s = bias_tile<false>(bias, a.reach, d0, lane), dp = f32x16(0.f);
+#pragma unroll
+                for (int u = 0; u < SQ; ++u) {
+                    s = mma<T>(row_piece<T, DP>(qt, 32 * n + m, u, h), kf[u], s);
+                    dp = mma<T>(row_piece<T, DP>(gt, 32 * n + m, u, h), vf[u], dp);
+                }
+                mask_tile<false>(s, nk - j0, nq - i0 - 32 * n, a.causal, d0, lane);
+                bool wild = false;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 t = *reinterpret_cast<const float4 *>(stats + BQ + 32 * n + 8 * q + 4 * h);
+                    const float v[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wild |= v[i] != kNegInf && fabsf(v[i]) > kWild;
+                }
+                wild = __any(wild);
+                f32x16 ds;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int at = 32 * n + 8 * q + 4 * h;
+                    const float4 l = *reinterpret_cast<const float4 *>(stats + at);
+                    const float4 e = *reinterpret_cast<const float4 *>(stats + 2 * BQ + at);
+                    const float ls[4] = {l.x, l.y, l.z, l.w}, dl[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 4 * q + i;
+                        if (wild) {
+                            const float top = stats[BQ + at + i];
+                            s[r] = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(a.c2, s[r] - top, -stats[3 * BQ + at + i]));
+                        } else {
+                            s[r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[r], -ls[i]));
+                        }
+                        ds[r] = s[r] * (dp[r] - dl[i]);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < Elem<T>::kSteps; ++u) {
+                    const uint4 p = piece_of<T>(s, u), d = piece_of<T>(ds, u);
+#pragma unroll
+                    for (int t = 0; t < DP / 32; ++t) {
+                        dv[t] = mma<T>(col_piece<T, DP>(gt, 32 * n, 32 * t, u, lane), p, dv[t]);
+                        dk[t] = mma<T>(col_piece<T, DP>(qt, 32 * n, 32 * t, u, lane), d, dk[t]);
+                    }
+                }
+            }
+        }
+    }
+    store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
+    store_rows<T, DP>(static_cast<T *>(b.grad_v), row, there, a.Hkv, hk, a.D, a.vec_o, dv, 1.f, lane);
+}
+
+// dT[b, h] from the workgroups' shares [slots, H, buckets], in a fixed order: 64
+// slots in turn by each of the workgroup's rows of threads, then the rows.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_grad_table(const float *__restrict__ part, int64_t nslots, int H, int buckets,
+                                                       T *__restrict__ out) {
+    __shared__ double sums[kBlock];
+    const int head = blockIdx.x, i = threadIdx.x & 15, r = threadIdx.x >> 4;
+    const int bk = blockIdx.y * 16 + i;
+    double t = 0;
+    if (bk < buckets)
+        for (int64_t s = r; s < nslots; s += kBlock / 16) t += part[(s * H + head) * buckets + bk];
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    if (r == 0 && bk < buckets) {
+        for (int k = 1; k < kBlock / 16; ++k) t += sums[16 * k + i];
+        out[(int64_t)bk * H + head] = T(static_cast<float>(t));
+    }
+}
+
+constexpr int64_t kMost = (int64_t(1) << 32) - 1;  // threads of a launch
+
+template <typename T, int DP, int WAVES, int BK>
+int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
+    const Args &a = b.f;
+    const int64_t nq = slots(a.Nq, a.B, 32 * WAVES), nk = slots(a.Nk, a.B, 32 * WAVES);
+    if (nq * a.H * 64 * WAVES > kMost || nk * a.Hkv * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
+    Carver c(ws);
+    float *delta = c.take<float>(a.Nq * a.H);
+    float *part = b.grad_table ? c.take<float>(nq * a.H * a.buckets) : nullptr;
+    const size_t tiles = 2 * BK * tile_stride<T, DP>() * sizeof(T), bias = (2 * a.reach + 1) * sizeof(float);
+    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES, tiles + bias * (part ? 1 + WAVES : 1), s>>>(
+        b, nq, delta, part);
+    PYG_LAUNCH_CHECK();
+    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv), 64 * WAVES, tiles + 4 * BK * sizeof(float) + bias,
+                                  s>>>(b, nk, delta);
+    PYG_LAUNCH_CHECK();
+    if (part) {
+        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), kBlock, 0, s>>>(part, nq, a.H, a.buckets,
+                                                                            static_cast<T *>(b.grad_table));
+        PYG_LAUNCH_CHECK();
+    }
+    return PYG_OK;
+}
+
+template <typename T, int DP>
+int by_waves(const BackwardArgs &b, void *ws, hipStream_t s) {
+    if (b.f.Nq <= 64 * b.f.B) return launch<T, DP, 1, 32>(b, ws, s);
+    return launch<T, DP, 4, 64>(b, ws, s);
+}
+
+template <typename T>
+int by_width(const BackwardArgs &b, void *ws, hipStream_t s) {
+    if (b.f.D <= 32) return by_waves<T, 32>(b, ws, s);
+    if (b.f.D <= 64) return by_waves<T, 64>(b, ws, s);
+    return by_waves<T, 128>(b, ws, s);
+}
+
+}  // namespace
+
+size_t backward_workspace(const Args &a) {
+    Carver c(nullptr);
+    c.take<float>(a.Nq * a.H);
+    c.take<float>(slots(a.Nq, a.B, 32) * a.H * a.buckets);  // the smallest tiles have the most slots
+    return align_up(c.used, 256);
+}
+
+int backward(const BackwardArgs &b, bool bf16, void *ws, hipStream_t s) {
+    return bf16 ? by_width<__bf16>(b, ws, s) : by_width<float>(b, ws, s);
+}
+
+}  // namespace attn
+}  // namespace pyg
