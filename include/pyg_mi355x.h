@@ -774,6 +774,75 @@ int pyg_global_attention_backward(const pyg_attention *a, const void *grad_out, 
                                   const void *v, const void *out, const float *stat, void *grad_q, void *grad_k,
                                   void *grad_v, void *grad_table, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- The norms around a block, with its gate and residual scale. */
+
+typedef enum { PYG_NORM_LAYER = 0, PYG_NORM_RMS = 1 } pyg_norm;
+
+/* u = norm(h; post), r = residual + scale * sigmoid(gate) * u, y = norm(r; pre), row by row:
+ * norm(x) = (x - mean) / sqrt(mean((x - mean)^2) + eps) * weight + bias (PYG_NORM_LAYER) or
+ * x / sqrt(mean(x^2) + eps) * weight + bias (PYG_NORM_RMS).
+ *   h, residual  [N, F] in dtype; gate [N, F], or [N] where gate_rows (one logit a row);
+ *   scale, post_weight, post_bias, weight, bias  fp32 [F].
+ * NULL leaves a part out: residual (0), gate (1), scale (1), post_weight (u = h),
+ * weight (no y), biases (0). F <= 8192. */
+typedef struct {
+    int dtype, norm;
+    int64_t N, F;
+    float eps;
+    const void *h, *residual, *gate;
+    int gate_rows;
+    const float *scale, *post_weight, *post_bias, *weight, *bias;
+} pyg_block_norm_args;
+
+/* r and y [N, F] in dtype, each rounded once (y is taken of the unrounded r; r may be NULL
+ * where y is made). codes and steps, or NULL: y as it was stored, in 8 bits (see
+ * pyg_activation_checkpoint). Statistics are fp32, two-pass. Deterministic.
+ * Errors: PYG_ERR_INVALID_ARG (bad dtype or norm, missing arrays, y without weight or
+ * weight without y, codes without y, eps < 0), PYG_ERR_UNSUPPORTED (F > 8192, N >= 2^31). */
+int pyg_block_norm(const pyg_block_norm_args *a, void *r, void *y, int8_t *codes, uint8_t *steps, void *stream);
+
+/* Workspace bytes needed by pyg_block_norm_backward. */
+int pyg_block_norm_backward_workspace(const pyg_block_norm_args *a, size_t *bytes);
+
+/* Gradients from grad_r and grad_y [N, F] (either may be NULL: zeros): grad_h, grad_residual
+ * [N, F], grad_gate in gate's shape, in dtype; grad_scale .. grad_bias fp32 [F]. NULL outputs
+ * are not made. Nothing of the forward is kept: the rows are normalised again. Deterministic.
+ * Errors: as above (a gradient of a part that is left out), PYG_ERR_WORKSPACE. */
+int pyg_block_norm_backward(const pyg_block_norm_args *a, const void *grad_r, const void *grad_y, void *grad_h,
+                            void *grad_residual, void *grad_gate, float *grad_scale, float *grad_post_weight,
+                            float *grad_post_bias, float *grad_weight, float *grad_bias, void *ws, size_t ws_bytes,
+                            void *stream);
+
+/* ---- Activations kept in 8 bits for the backward pass. */
+
+/* codes int8 [N, 32 ceil(F / 32)] and steps uint8 [N, ceil(F / 32)] of x [N, F]: every block
+ * of 32 features of a row shares a step 2^(steps - 127), the smallest power of two that
+ * leaves the block's largest magnitude below 127.5 steps (2^-126 at least); a code is x / step
+ * rounded to the nearest integer, ties to even; codes past F are 0. A block that holds an
+ * infinity or NaN has steps = 255 and comes back as NaN. Exact up to that one rounding.
+ *   x fp32 or bf16; codes 16-byte aligned.
+ * Errors: PYG_ERR_INVALID_ARG, PYG_ERR_UNSUPPORTED (N >= 2^31, F >= 2^24). */
+int pyg_activation_checkpoint(const void *x, int dtype, int64_t N, int64_t F, int8_t *codes, uint8_t *steps,
+                              void *stream);
+
+/* x [N, F] = codes * 2^(steps - 127) in dtype (exact in fp32 and in bf16). */
+int pyg_checkpoint_restore(const int8_t *codes, const uint8_t *steps, int64_t N, int64_t F, void *x, int dtype,
+                           void *stream);
+
+/* Workspace bytes needed by pyg_dense_transform_backward. */
+int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int64_t Fo, size_t *bytes);
+
+/* Gradients of out = X Theta (pyg_dense_transform) where X was kept in 8 bits:
+ *   grad_theta [Fi, Fo] = X^T G with X from codes and steps (NULL with grad_theta NULL);
+ *   grad_x     [N, Fi]  = G Theta^T (theta [Fi, Fo] row-major, or NULL with grad_x NULL);
+ * G = grad_out [N, Fo], theta and both results in dtype, fp32 accumulation (fp32
+ * operands enter the weight gradient as three bf16 parts each, which hold all their bits).
+ * Deterministic. Errors: PYG_ERR_INVALID_ARG, PYG_ERR_UNSUPPORTED (N >= 2^31, Fi or Fo >=
+ * 2^24), PYG_ERR_WORKSPACE. */
+int pyg_dense_transform_backward(const void *grad_out, int dtype, int64_t N, int64_t Fo, const void *theta, int64_t Fi,
+                                 const int8_t *codes, const uint8_t *steps, void *grad_x, void *grad_theta, void *ws,
+                                 size_t ws_bytes, void *stream);
+
 /* Workspace bytes needed by pyg_global_pool. */
 int pyg_global_pool_workspace(int dtype, int64_t N, int64_t F, int64_t B, int aggr, size_t *bytes);
 

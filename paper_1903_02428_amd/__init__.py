@@ -62,7 +62,15 @@ from .binding import (  # noqa: F401
     validate_coo,
 )
 from .transformer import (  # noqa: F401
+    BlockNorm,
+    Checkpoint,
+    DenseTransform,
     GlobalAttention,
+    activation_checkpoint,
+    block_norm,
+    block_norm_backward,
+    checkpoint_restore,
+    dense_transform_backward,
     global_attention,
     global_attention_backward,
     global_attention_workspace_bytes,

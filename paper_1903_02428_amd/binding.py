@@ -38,6 +38,9 @@ EXPORTED = [
     "pyg_gat_forward_workspace", "pyg_gat_forward", "pyg_gat_backward_workspace", "pyg_gat_backward",
     "pyg_global_attention_workspace", "pyg_global_attention", "pyg_global_attention_backward_workspace",
     "pyg_global_attention_backward",
+    "pyg_block_norm", "pyg_block_norm_backward_workspace", "pyg_block_norm_backward",
+    "pyg_activation_checkpoint", "pyg_checkpoint_restore", "pyg_dense_transform_backward_workspace",
+    "pyg_dense_transform_backward",
 ]
 
 
@@ -70,6 +73,13 @@ class _Attention(ctypes.Structure):
         [("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("causal", ctypes.c_int), ("table", ctypes.c_void_p),
          ("bucket", ctypes.c_void_p), ("buckets", ctypes.c_int64), ("reach", ctypes.c_int64),
          ("zero_rest", ctypes.c_int)]
+
+
+class _BlockNorm(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("norm", ctypes.c_int), ("N", ctypes.c_int64), ("F", ctypes.c_int64),
+                ("eps", ctypes.c_float), ("h", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_rows", ctypes.c_int)] + \
+        [(n, ctypes.c_void_p) for n in ("scale", "post_weight", "post_bias", "weight", "bias")]
 
 
 _lib = None
@@ -159,6 +169,13 @@ def library() -> ctypes.CDLL:
             "pyg_global_attention_backward_workspace": [ctypes.POINTER(_Attention), sz],
             "pyg_global_attention_backward": [ctypes.POINTER(_Attention), p, p, p, p, p, p, p, p, p, p, p,
                                               ctypes.c_size_t, p],
+            "pyg_block_norm": [ctypes.POINTER(_BlockNorm), p, p, p, p, p],
+            "pyg_block_norm_backward_workspace": [ctypes.POINTER(_BlockNorm), sz],
+            "pyg_block_norm_backward": [ctypes.POINTER(_BlockNorm), p, p, p, p, p, p, p, p, p, p, p, ctypes.c_size_t, p],
+            "pyg_activation_checkpoint": [p, i32, i64, i64, p, p, p],
+            "pyg_checkpoint_restore": [p, p, i64, i64, p, i32, p],
+            "pyg_dense_transform_backward_workspace": [i32, i64, i64, i64, sz],
+            "pyg_dense_transform_backward": [p, i32, i64, i64, p, i64, p, p, p, p, p, ctypes.c_size_t, p],
             "pyg_validate_coo": [p, i64, i64, p, p],
             "pyg_validate_batch": [p, i64, i64, p, p],
         }

@@ -1,0 +1,350 @@
+// Activations in 8 bits and back, and the gradients of the dense transform from
+// them: dTheta = X^T G on the matrix cores with X straight from its codes.
+//
+// A code times its step is a bf16 value, so X enters v_mfma_f32_32x32x16_bf16
+// unrounded; bf16 gradients too. fp32 gradients are cut into three bf16 parts
+// (their first, second and last 8 significant bits), three exact products instead of fp32 instructions at a sixteenth of the rate each.
+// The products contract over the rows n, which both operands hold as rows: tiles of
+// 32 rows go to LDS as they lie, and the transposing LDS read makes the operands.
+#include "attn_tiles.hpp"
+#include "eight_bit.hpp"
+
+namespace pyg {
+namespace {
+
+using attn::f32x16;
+
+// One thread a piece of 16 bytes of x: E lanes' neighbours share a block of 32.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_checkpoint(const T *__restrict__ x, int64_t N, int F, int pieces, bool vec,
+                                                       uint8_t *__restrict__ codes, uint8_t *__restrict__ steps) {
+    constexpr int E = 16 / sizeof(T);
+    const int64_t all = N * pieces, step = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < all; i += step) {  // pieces * E is a multiple of 32:
+        const int64_t row = i / pieces;                                                 // blocks stay in 8 or 4 lanes
+        const int f = static_cast<int>(i - row * pieces) * E;
+        attn::Piece<T> p;
+        p.u = attn::load_piece<T>(x + row * F, f, F, vec, true);
+        float v[E];
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = static_cast<float>(p.v[e]);
+            const uint32_t m = eight::magnitude(v[e]);
+            top = m > top ? m : top;
+        }
+#pragma unroll
+        for (int o = 1; o < 32 / E; o <<= 1) {
+            const uint32_t m = __shfl_xor(top, o);
+            top = m > top ? m : top;
+        }
+        const uint32_t ex = eight::step_of(top);
+        const float inv = eight::step_inverse(ex);
+        uint32_t q[E / 4];
+#pragma unroll
+        for (int j = 0; j < E / 4; ++j)
+            q[j] = eight::code(v[4 * j], inv, ex) | eight::code(v[4 * j + 1], inv, ex) << 8 |
+                   eight::code(v[4 * j + 2], inv, ex) << 16 | eight::code(v[4 * j + 3], inv, ex) << 24;
+        uint8_t *c = codes + i * E;
+        if constexpr (E == 4) *reinterpret_cast<uint32_t *>(c) = q[0];
+        else *reinterpret_cast<uint2 *>(c) = make_uint2(q[0], q[E / 4 - 1]);
+        if (f % 32 == 0) steps[i * E / 32] = static_cast<uint8_t>(ex);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_restore(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ steps,
+                                                    int64_t N, int F, int pieces, bool vec, T *__restrict__ x) {
+    constexpr int E = 16 / sizeof(T);
+    const int64_t all = N * pieces, step = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < all; i += step) {
+        const int64_t row = i / pieces;
+        const int f = static_cast<int>(i - row * pieces) * E;
+        if (f >= F) continue;
+        const float s = eight::step_value(steps[i * E / 32]);
+        attn::Piece<T> p;
+#pragma unroll
+        for (int j = 0; j < E / 4; ++j) {
+            float v[4];
+            eight::unpack(*reinterpret_cast<const uint32_t *>(codes + i * E + 4 * j), v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p.v[4 * j + e] = T(v[e] * s);
+        }
+        T *o = x + row * F + f;
+        if (vec) {
+            *reinterpret_cast<uint4 *>(o) = p.u;
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (f + e < F) o[e] = p.v[e];
+        }
+    }
+}
+
+// ------------------------------------------------------------ dTheta = X^T G
+
+constexpr int kTileI = 128, kTileO = 128, kTileN = 32;
+typedef __bf16 bf16;
+constexpr int kStride = attn::tile_stride<bf16, 128>();
+
+// A workgroup owns 128 x 128 of dTheta and every splits-th tile of 32 rows. PARTS
+// bf16 parts of G (1: bf16 G, 3: fp32 G).
+template <typename T, int PARTS>
+__global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ steps,
+                                                       const T *__restrict__ g, int64_t N, int Fi, int Fo, int blocks,
+                                                       bool vec, int splits, float *__restrict__ part) {
+    constexpr int E = 16 / sizeof(T), GP = kTileN * kTileO / E / kBlock;
+    __shared__ __align__(16) bf16 xt[kTileN * kStride];
+    __shared__ __align__(16) bf16 gt[PARTS][kTileN * kStride];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tiles_o = (Fo + kTileO - 1) / kTileO;
+    const int sp = blockIdx.x % splits, tile = blockIdx.x / splits;
+    const int i0 = tile / tiles_o * kTileI, o0 = tile % tiles_o * kTileO;
+    const int wi = wave / 2 * 64, wo = wave % 2 * 64;  // the wavefront's 64 x 64
+    const int64_t width = (int64_t)blocks * 32;
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[a][b] = f32x16(0.f);
+
+    // 16 codes and their step, and GP pieces of G a thread
+    const int xr = threadIdx.x / 8, xc = threadIdx.x % 8 * 16;
+    uint4 cx;
+    uint32_t ex;
+    uint4 cg[GP];
+    auto load = [&](int64_t n0) {
+        cx = make_uint4(0, 0, 0, 0);
+        ex = 1;
+        if (n0 + xr < N && i0 + xc < width) {
+            cx = *reinterpret_cast<const uint4 *>(codes + (n0 + xr) * width + i0 + xc);
+            ex = steps[(n0 + xr) * blocks + (i0 + xc) / 32];
+        }
+#pragma unroll
+        for (int j = 0; j < GP; ++j) {
+            const int p = j * kBlock + threadIdx.x, r = p / (kTileO / E), c = p % (kTileO / E) * E;
+            cg[j] = attn::load_piece<T>(g + (n0 + r) * Fo, o0 + c, Fo, vec, n0 + r < N);
+        }
+    };
+    auto store = [&]() {
+        const float s = eight::step_value(ex);
+        const uint32_t w[4] = {cx.x, cx.y, cx.z, cx.w};
+        uint32_t o[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float v[4];
+            eight::unpack(w[j], v);
+            o[2 * j] = attn::pack_bf16(v[0] * s, v[1] * s), o[2 * j + 1] = attn::pack_bf16(v[2] * s, v[3] * s);  // exact
+        }
+        uint4 *x = reinterpret_cast<uint4 *>(xt + xr * kStride + xc);
+        x[0] = make_uint4(o[0], o[1], o[2], o[3]), x[1] = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+        for (int j = 0; j < GP; ++j) {
+            const int p = j * kBlock + threadIdx.x, r = p / (kTileO / E), c = p % (kTileO / E) * E;
+            if constexpr (PARTS == 1) {
+                *reinterpret_cast<uint4 *>(gt[0] + r * kStride + c) = cg[j];
+            } else {
+                attn::Piece<T> v;
+                v.u = cg[j];
+                float f[4] = {v.v[0], v.v[1], v.v[2], v.v[3]};
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) {
+                    uint32_t b[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        b[e] = __float_as_uint(f[e]) & 0xFFFF0000u;
+                        // an infinity or NaN is all in the first part
+                        f[e] = (b[e] & 0x7F800000u) == 0x7F800000u ? 0.f : f[e] - __uint_as_float(b[e]);
+                    }
+                    *reinterpret_cast<uint2 *>(gt[k] + r * kStride + c) = make_uint2(b[0] >> 16 | b[1], b[2] >> 16 | b[3]);
+                }
+            }
+        }
+    };
+    int64_t n0 = (int64_t)sp * kTileN;
+    if (n0 < N) load(n0);
+    for (; n0 < N; n0 += (int64_t)splits * kTileN) {
+        __syncthreads();
+        store();
+        __syncthreads();
+        if (n0 + (int64_t)splits * kTileN < N) load(n0 + (int64_t)splits * kTileN);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            uint4 a[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) a[t] = attn::col_piece<bf16, 128>(xt, 0, wi + 32 * t, u, lane);
+#pragma unroll
+            for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint4 y = attn::col_piece<bf16, 128>(gt[k], 0, wo + 32 * b, u, lane);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) acc[t][b] = attn::mma<bf16>(a[t], y, acc[t][b]);
+                }
+        }
+    }
+    float *p = part + (int64_t)sp * Fi * Fo;
+    const int h = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int o = o0 + wo + 32 * b + (lane & 31);
+            if (o >= Fo) continue;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = i0 + wi + 32 * t + 8 * (r >> 2) + 4 * h + (r & 3);
+                if (i < Fi) p[(int64_t)i * Fo + o] = acc[t][b][r];
+            }
+        }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_join_theta(const float *__restrict__ part, int64_t n, int splits,
+                                                       T *__restrict__ out) {
+    // 32 values a workgroup, 8 threads a value
+    __shared__ float lds[8][32];
+    const int i = threadIdx.x & 31, r = threadIdx.x >> 5;
+    const int64_t at = (int64_t)blockIdx.x * 32 + i;
+    float v = 0.f;
+    if (at < n)
+#pragma unroll 8
+        for (int s = r; s < splits; s += 8) v += part[(int64_t)s * n + at];
+    lds[r][i] = v;
+    __syncthreads();
+    if (r == 0 && at < n) {
+        for (int k = 1; k < 8; ++k) v += lds[k][i];
+        out[at] = T(v);
+    }
+}
+
+// Theta [Fi, Fo] -> Theta^T [Fo, Fi].
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_transpose(const T *__restrict__ in, int64_t Fi, int64_t Fo, T *__restrict__ out) {
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < Fi * Fo; i += (int64_t)gridDim.x * kBlock)
+        out[i] = in[i % Fi * Fo + i / Fi];
+}
+
+constexpr int64_t kMax32 = int64_t(1) << 31, kMaxF = int64_t(1) << 24;
+
+// Row ranges of dTheta: two workgroups a CU, 256 rows or more each.
+int splits_of(int64_t N, int64_t Fi, int64_t Fo) {
+    const int64_t tiles = ((Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO);
+    int64_t s = 512 / tiles, most = N / 256;
+    s = s < most ? s : most;
+    return static_cast<int>(s < 1 ? 1 : s);
+}
+
+bool aligned(const void *p, int64_t row_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && row_bytes % 16 == 0; }
+
+template <typename T>
+int theta_grad(const T *g, int64_t N, int Fo, int Fi, const int8_t *codes, const uint8_t *steps, T *out, float *part,
+               hipStream_t s) {
+    const int splits = splits_of(N, Fi, Fo), blocks = (Fi + 31) / 32;
+    const int64_t tiles = ((int64_t)(Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO), n = (int64_t)Fi * Fo;
+    if (tiles * splits * kBlock >= (int64_t(1) << 32) || n / 32 * kBlock >= (int64_t(1) << 32)) return PYG_ERR_UNSUPPORTED;
+    k_theta_grad<T, sizeof(T) == 2 ? 1 : 3><<<static_cast<unsigned>(tiles * splits), kBlock, 0, s>>>(
+        reinterpret_cast<const uint8_t *>(codes), steps, g, N, Fi, Fo, blocks, aligned(g, (int64_t)Fo * sizeof(T)), splits, part);
+    PYG_LAUNCH_CHECK();
+    k_join_theta<T><<<static_cast<unsigned>((n + 31) / 32), kBlock, 0, s>>>(part, n, splits, out);
+    PYG_LAUNCH_CHECK();
+    return PYG_OK;
+}
+
+}  // namespace
+}  // namespace pyg
+
+using namespace pyg;
+
+extern "C" int pyg_activation_checkpoint(const void *x, int dtype, int64_t N, int64_t F, int8_t *codes, uint8_t *steps,
+                                         void *stream) {
+    if ((dtype != PYG_F32 && dtype != PYG_BF16) || N < 0 || F < 1) return PYG_ERR_INVALID_ARG;
+    if (N >= kMax32 || F >= kMaxF) return PYG_ERR_UNSUPPORTED;
+    if (N == 0) return PYG_OK;
+    if (!x || !codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16) return PYG_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int width = static_cast<int>((F + 31) / 32 * 32), f = static_cast<int>(F);
+    uint8_t *c = reinterpret_cast<uint8_t *>(codes);
+    const unsigned grid = grid_for(N * (width / (dtype == PYG_BF16 ? 8 : 4)), kBlock, 1 << 16);
+    if (dtype == PYG_BF16)
+        k_checkpoint<__bf16><<<grid, kBlock, 0, s>>>(static_cast<const __bf16 *>(x), N, f, width / 8, aligned(x, F * 2), c, steps);
+    else
+        k_checkpoint<float><<<grid, kBlock, 0, s>>>(static_cast<const float *>(x), N, f, width / 4, aligned(x, F * 4), c, steps);
+    PYG_LAUNCH_CHECK();
+    return PYG_OK;
+}
+
+extern "C" int pyg_checkpoint_restore(const int8_t *codes, const uint8_t *steps, int64_t N, int64_t F, void *x, int dtype,
+                                      void *stream) {
+    if ((dtype != PYG_F32 && dtype != PYG_BF16) || N < 0 || F < 1) return PYG_ERR_INVALID_ARG;
+    if (N >= kMax32 || F >= kMaxF) return PYG_ERR_UNSUPPORTED;
+    if (N == 0) return PYG_OK;
+    if (!x || !codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16) return PYG_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int width = static_cast<int>((F + 31) / 32 * 32), f = static_cast<int>(F);
+    const uint8_t *c = reinterpret_cast<const uint8_t *>(codes);
+    const unsigned grid = grid_for(N * (width / (dtype == PYG_BF16 ? 8 : 4)), kBlock, 1 << 16);
+    if (dtype == PYG_BF16)
+        k_restore<__bf16><<<grid, kBlock, 0, s>>>(c, steps, N, f, width / 8, aligned(x, F * 2), static_cast<__bf16 *>(x));
+    else
+        k_restore<float><<<grid, kBlock, 0, s>>>(c, steps, N, f, width / 4, aligned(x, F * 4), static_cast<float *>(x));
+    PYG_LAUNCH_CHECK();
+    return PYG_OK;
+}
+
+namespace {
+
+struct Layout {
+    size_t bytes;
+    void *theta_t, *dense;
+    size_t dense_bytes;
+    float *part;
+};
+int layout(int dtype, int64_t N, int64_t Fi, int64_t Fo, void *ws, Layout *l) {
+    if ((dtype != PYG_F32 && dtype != PYG_BF16) || N < 0 || Fi < 1 || Fo < 1) return PYG_ERR_INVALID_ARG;
+    if (N >= kMax32 || Fi >= kMaxF || Fo >= kMaxF) return PYG_ERR_UNSUPPORTED;
+    PYG_TRY(pyg_dense_transform_workspace(Fo, Fi, &l->dense_bytes));
+    Carver c(ws);
+    l->part = c.take<float>(static_cast<size_t>(splits_of(N, Fi, Fo)) * Fi * Fo);
+    l->theta_t = c.take<char>(static_cast<size_t>(Fi) * Fo * (dtype == PYG_BF16 ? 2 : 4));
+    l->dense = c.take<char>(l->dense_bytes);
+    l->bytes = align_up(c.used, 256);
+    return PYG_OK;
+}
+
+}  // namespace
+
+extern "C" int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int64_t Fo, size_t *bytes) {
+    Layout l{};
+    if (!bytes) return PYG_ERR_INVALID_ARG;
+    PYG_TRY(layout(dtype, N, Fi, Fo, nullptr, &l));
+    *bytes = l.bytes;
+    return PYG_OK;
+}
+
+extern "C" int pyg_dense_transform_backward(const void *grad_out, int dtype, int64_t N, int64_t Fo, const void *theta,
+                                            int64_t Fi, const int8_t *codes, const uint8_t *steps, void *grad_x,
+                                            void *grad_theta, void *ws, size_t ws_bytes, void *stream) {
+    Layout l{};
+    PYG_TRY(layout(dtype, N, Fi, Fo, ws, &l));
+    if (N > 0 && !grad_out) return PYG_ERR_INVALID_ARG;
+    if (grad_x && !theta) return PYG_ERR_INVALID_ARG;
+    if (grad_theta && N > 0 && (!codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16)) return PYG_ERR_INVALID_ARG;
+    if (ws_bytes < l.bytes || !ws) return PYG_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (grad_x && N > 0) {
+        const unsigned grid = grid_for(Fi * Fo, kBlock, 4096);
+        if (dtype == PYG_BF16)
+            k_transpose<uint16_t><<<grid, kBlock, 0, s>>>(static_cast<const uint16_t *>(theta), Fi, Fo, static_cast<uint16_t *>(l.theta_t));
+        else
+            k_transpose<uint32_t><<<grid, kBlock, 0, s>>>(static_cast<const uint32_t *>(theta), Fi, Fo, static_cast<uint32_t *>(l.theta_t));
+        PYG_LAUNCH_CHECK();
+        PYG_TRY(pyg_dense_transform(grad_out, dtype, N, Fo, l.theta_t, Fi, grad_x, dtype, l.dense, l.dense_bytes, stream));
+    }
+    if (!grad_theta) return PYG_OK;
+    const int fi = static_cast<int>(Fi), fo = static_cast<int>(Fo);
+    return dtype == PYG_BF16 ? theta_grad(static_cast<const __bf16 *>(grad_out), N, fo, fi, codes, steps,
+                                          static_cast<__bf16 *>(grad_theta), l.part, s)
+                             : theta_grad(static_cast<const float *>(grad_out), N, fo, fi, codes, steps,
+                                          static_cast<float *>(grad_theta), l.part, s);
+}

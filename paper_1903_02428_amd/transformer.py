@@ -1,14 +1,19 @@
 """The parts of a graph transformer's block (ctypes marshalling only): attention
-among the nodes of each graph with a learned bias by relative position."""
+among the nodes of each graph with a learned bias by relative position, the norms around
+a block with its gate and residual scale, and activations kept in 8 bits."""
 from __future__ import annotations
 
 import contextlib
 import ctypes
 import math
+from dataclasses import dataclass
 
 import torch
 
-from .binding import DTYPE, _Attention, _check, _need_cuda, _ptr, _stream, _workspace, library
+from .binding import (DTYPE, _aligned16, _Attention, _BlockNorm, _check, _need_cuda, _ptr, _size, _stream, _workspace,
+                      dense_transform, library)
+
+NORM = {"layer": 0, "rms": 1}
 
 
 def _on(device):
@@ -204,3 +209,264 @@ class GlobalAttention(torch.autograd.Function):
         grads = global_attention_backward(grad_out.to(q.dtype).contiguous(), qc, kc, vc, out.contiguous(), stat, ptr, k_ptr,
                                           tc, buckets, ctx.causal, ctx.scale, need_grad_table=ctx.needs_input_grad[3])
         return tuple(g if need else None for g, need in zip(grads, ctx.needs_input_grad)) + (None,) * 5
+
+
+# ------------------------------------------------------- activations in 8 bits
+
+
+@dataclass
+class Checkpoint:
+    """A matrix [N, F] kept in 8 bits (activation_checkpoint): int8 codes, 32 features of
+    a row sharing a power-of-two step."""
+    codes: torch.Tensor  # int8 [N, 32 * blocks]
+    steps: torch.Tensor  # uint8 [N, blocks]: exponent of the step + 127
+    F: int
+    dtype: torch.dtype   # what it was made from
+
+    @property
+    def N(self) -> int:
+        return self.steps.shape[0]
+
+
+def _new_checkpoint(N: int, F: int, dtype, device) -> Checkpoint:
+    blocks = -(-F // 32)
+    return Checkpoint(torch.empty((N, blocks * 32), dtype=torch.int8, device=device),
+                      torch.empty((N, blocks), dtype=torch.uint8, device=device), F, dtype)
+
+
+def _checked(kept: Checkpoint, device=None):
+    _need_cuda("codes", kept.codes, torch.int8, 2)
+    _need_cuda("steps", kept.steps, torch.uint8, 2)
+    blocks = -(-kept.F // 32)
+    if kept.F < 1 or kept.steps.shape[1] != blocks or tuple(kept.codes.shape) != (kept.N, blocks * 32):
+        raise ValueError("codes must be [N, 32 * blocks] and steps [N, blocks] with blocks = ceil(F / 32)")
+    if not _aligned16(kept.codes):
+        raise ValueError("codes must be 16-byte aligned")
+    _same_device(device or kept.codes.device, codes=kept.codes, steps=kept.steps)
+    return kept
+
+
+def activation_checkpoint(x: torch.Tensor, out: Checkpoint | None = None) -> Checkpoint:
+    """x [N, F] (float32 or bfloat16) in 8 bits: every 32 features of a row share a step, the smallest
+    power of two that leaves the largest of them below 127.5 steps; a code is the
+    nearest multiple (ties to even). Blocks with an infinity or NaN come back as NaN."""
+    _need_cuda("x", x, None, 2)
+    if x.dtype not in DTYPE:
+        raise ValueError("x must be float32 or bfloat16")
+    N, F = x.shape
+    if F < 1:
+        raise ValueError("x must have features")
+    if out is None:
+        out = _new_checkpoint(N, F, x.dtype, x.device)
+    elif (out.N, out.F, out.dtype) != (N, F, x.dtype):
+        raise ValueError("out is the checkpoint of another shape or type")
+    _checked(out, x.device)
+    with _on(x.device):
+        _check(library().pyg_activation_checkpoint(_ptr(x), DTYPE[x.dtype], N, F, _ptr(out.codes), _ptr(out.steps),
+                                                   _stream(x.device)), "pyg_activation_checkpoint")
+    return out
+
+
+def checkpoint_restore(kept: Checkpoint, dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The matrix that a checkpoint stands for, exactly (in float32 or bfloat16)."""
+    _checked(kept)
+    dtype = (kept.dtype if out is None else out.dtype) if dtype is None else dtype
+    if dtype not in DTYPE:
+        raise ValueError("dtype must be float32 or bfloat16")
+    dev = kept.codes.device
+    if out is None:
+        out = torch.empty((kept.N, kept.F), dtype=dtype, device=dev)
+    else:
+        _need_cuda("out", out, dtype, 2)
+        if tuple(out.shape) != (kept.N, kept.F):
+            raise ValueError("out must be [N, F]")
+        _same_device(dev, out=out)
+    with _on(dev):
+        _check(library().pyg_checkpoint_restore(_ptr(kept.codes), _ptr(kept.steps), kept.N, kept.F, _ptr(out),
+                                                DTYPE[dtype], _stream(dev)), "pyg_checkpoint_restore")
+    return out
+
+
+def dense_transform_backward(grad_out: torch.Tensor, theta: torch.Tensor, kept: Checkpoint, need_grad_x: bool = True,
+                             need_grad_theta: bool = True, workspace: torch.Tensor | None = None):
+    """Gradients of dense_transform(x, theta) from grad_out [N, Fo] and x kept in 8 bits:
+    (grad_x = grad_out theta^T or None, grad_theta = x^T grad_out or None), in theta's type."""
+    lib = library()
+    _need_cuda("grad_out", grad_out, None, 2)
+    if grad_out.dtype not in DTYPE:
+        raise ValueError("grad_out must be float32 or bfloat16")
+    _need_cuda("theta", theta, grad_out.dtype, 2)
+    dev = grad_out.device
+    _checked(kept, dev)
+    (N, Fo), Fi = grad_out.shape, theta.shape[0]
+    if theta.shape[1] != Fo or kept.N != N or kept.F != Fi:
+        raise ValueError("grad_out must be [N, Fo], theta [Fi, Fo] and the checkpoint [N, Fi]")
+    if Fo < 1:
+        raise ValueError("theta must have columns")
+    _same_device(dev, theta=theta, workspace=workspace)
+    gx = torch.empty((N, Fi), dtype=theta.dtype, device=dev) if need_grad_x else None
+    gt = torch.empty_like(theta) if need_grad_theta else None
+    with _on(dev):
+        nbytes = _size(lib.pyg_dense_transform_backward_workspace, DTYPE[theta.dtype], N, Fi, Fo)
+        if workspace is None or workspace.numel() < nbytes:
+            workspace = _workspace(nbytes, dev)
+        _check(lib.pyg_dense_transform_backward(_ptr(grad_out), DTYPE[theta.dtype], N, Fo, _ptr(theta), Fi,
+                                                _ptr(kept.codes), _ptr(kept.steps), _ptr(gx), _ptr(gt), _ptr(workspace),
+                                                workspace.numel(), _stream(dev)), "pyg_dense_transform_backward")
+    return gx, gt
+
+
+class DenseTransform(torch.autograd.Function):
+    """Differentiable dense_transform whose input is kept in 8 bits for the backward: the
+    gradient of theta is that of the kept values. Use as DenseTransform.apply(x, theta,
+    kept): `kept` is x's checkpoint where there is one (block_norm makes it with y), else it is made
+    here. x, theta and the result have one type."""
+
+    @staticmethod
+    def forward(ctx, x, theta, kept: Checkpoint | None = None):
+        xc, tc = x.detach().contiguous(), theta.detach().contiguous()
+        ctx.F = None
+        if ctx.needs_input_grad[1]:
+            kept = activation_checkpoint(xc) if kept is None else kept
+            if (kept.N, kept.F) != tuple(x.shape):
+                raise ValueError("kept must be the checkpoint of x")
+            ctx.F = kept.F
+        ctx.shape = tuple(x.shape)
+        out = dense_transform(xc, tc, x.dtype)
+        ctx.save_for_backward(theta, *((kept.codes, kept.steps) if ctx.F else ()))
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        theta, *held = ctx.saved_tensors
+        g, t = grad_out.to(theta.dtype).contiguous(), theta.detach().contiguous()
+        kept = Checkpoint(*held, ctx.F, theta.dtype) if ctx.F else None
+        if kept is None:  # the weights need no gradient: nothing was kept
+            return (dense_transform(g, t.t().contiguous(), theta.dtype), None, None)
+        gx, gt = dense_transform_backward(g, t, kept, ctx.needs_input_grad[0], True)
+        return gx, gt, None
+
+
+# ------------------------------------------------------- norms around a block
+
+
+def _norm_args(h, residual, gate, scale, post_weight, post_bias, weight, bias, norm, eps) -> _BlockNorm:
+    _need_cuda("h", h, None, 2)
+    if h.dtype not in DTYPE:
+        raise ValueError("h must be float32 or bfloat16")
+    if norm not in NORM:
+        raise ValueError("norm must be 'layer' or 'rms'")
+    if not eps >= 0:
+        raise ValueError("eps must not be negative")
+    N, F = h.shape
+    if F < 1:
+        raise ValueError("h must have features")
+    if residual is not None:
+        _need_cuda("residual", residual, h.dtype, 2)
+        if residual.shape != h.shape:
+            raise ValueError("residual must have h's shape")
+    if gate is not None:
+        _need_cuda("gate", gate, h.dtype, 2)
+        if gate.shape[0] != N or gate.shape[1] not in (1, F):
+            raise ValueError("gate must be [N, F] or [N, 1]")
+    for name, t in (("scale", scale), ("post_weight", post_weight), ("post_bias", post_bias), ("weight", weight),
+                    ("bias", bias)):
+        if t is not None:
+            _need_cuda(name, t, torch.float32, 1)
+            if t.shape[0] != F:
+                raise ValueError(f"{name} must be [F]")
+    if (post_bias is not None and post_weight is None) or (bias is not None and weight is None):
+        raise ValueError("a bias needs its weight")
+    _same_device(h.device, residual=residual, gate=gate, scale=scale, post_weight=post_weight, post_bias=post_bias,
+                 weight=weight, bias=bias)
+    return _BlockNorm(DTYPE[h.dtype], NORM[norm], N, F, eps, _ptr(h), _ptr(residual), _ptr(gate),
+                      int(gate is not None and gate.shape[1] == 1), _ptr(scale), _ptr(post_weight), _ptr(post_bias),
+                      _ptr(weight), _ptr(bias))
+
+
+def block_norm(h: torch.Tensor, residual: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+               scale: torch.Tensor | None = None, post_weight: torch.Tensor | None = None,
+               post_bias: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+               bias: torch.Tensor | None = None, norm: str = "layer", eps: float = 1e-5, checkpoint: bool = False):
+    """What lies between two blocks of a transformer, in one pass over the rows: with h the
+    first block's result and `residual` its input,
+        u = norm(h) * post_weight + post_bias           (h without post_weight)
+        r = residual + scale * sigmoid(gate) * u
+        y = norm(r) * weight + bias                     (None without weight)
+    h, residual [N, F], gate [N, F] or [N, 1] in one type (float32 or bfloat16), scale, weights and
+    biases float32 [F]; norm "layer" or "rms"; F <= 8192. Returns (r, y, kept): kept is y's
+    8-bit checkpoint with `checkpoint`, else None. Where all that is asked is a norm (no
+    residual, gate, scale or post_weight), r is h itself."""
+    a = _norm_args(h, residual, gate, scale, post_weight, post_bias, weight, bias, norm, eps)
+    if checkpoint and weight is None:
+        raise ValueError("a checkpoint is made of y: weight is needed")
+    plain = residual is None and gate is None and scale is None and post_weight is None
+    r = h if plain else torch.empty_like(h)
+    y = torch.empty_like(h) if weight is not None else None
+    kept = _new_checkpoint(a.N, a.F, h.dtype, h.device) if checkpoint else None
+    if plain and y is None:
+        return r, None, None
+    with _on(h.device):
+        _check(library().pyg_block_norm(ctypes.byref(a), None if plain else _ptr(r), _ptr(y),
+                                        _ptr(kept.codes) if kept else None, _ptr(kept.steps) if kept else None,
+                                        _stream(h.device)), "pyg_block_norm")
+    return r, y, kept
+
+
+def block_norm_backward(grad_r: torch.Tensor | None, grad_y: torch.Tensor | None, h, residual=None, gate=None, scale=None,
+                        post_weight=None, post_bias=None, weight=None, bias=None, norm: str = "layer", eps: float = 1e-5,
+                        need: tuple | None = None, workspace: torch.Tensor | None = None):
+    """Gradients of block_norm for its eight tensors, in their order (None where one is
+    missing or not needed), from the gradients of r and y (None: zeros)."""
+    lib = library()
+    a = _norm_args(h, residual, gate, scale, post_weight, post_bias, weight, bias, norm, eps)
+    for name, g in (("grad_r", grad_r), ("grad_y", grad_y)):
+        if g is not None:
+            _need_cuda(name, g, h.dtype, 2)
+            if g.shape != h.shape:
+                raise ValueError(f"{name} must have h's shape")
+    if grad_r is None and grad_y is None:
+        raise ValueError("need grad_r or grad_y")
+    if grad_y is not None and weight is None:
+        raise ValueError("there is no y without weight")
+    _same_device(h.device, grad_r=grad_r, grad_y=grad_y, workspace=workspace)
+    tensors = (h, residual, gate, scale, post_weight, post_bias, weight, bias)
+    need = need or (True,) * 8
+    grads = tuple(torch.empty_like(t) if t is not None and n else None for t, n in zip(tensors, need))
+    with _on(h.device):
+        nbytes = _bytes(lib.pyg_block_norm_backward_workspace, a)
+        if workspace is None or workspace.numel() < nbytes:
+            workspace = _workspace(nbytes, h.device)
+        _check(lib.pyg_block_norm_backward(ctypes.byref(a), _ptr(grad_r), _ptr(grad_y), *[_ptr(g) for g in grads],
+                                           _ptr(workspace), workspace.numel(), _stream(h.device)),
+               "pyg_block_norm_backward")
+    return grads
+
+
+class BlockNorm(torch.autograd.Function):
+    """Differentiable block_norm. Use as BlockNorm.apply(h, residual, gate, scale, post_weight,
+    post_bias, weight, bias, norm, eps, checkpoint), None for the parts that are left out;
+    returns (r, y, kept). Nothing but the inputs is kept for the backward."""
+
+    @staticmethod
+    def forward(ctx, h, residual=None, gate=None, scale=None, post_weight=None, post_bias=None, weight=None, bias=None,
+                norm: str = "layer", eps: float = 1e-5, checkpoint: bool = False):
+        tensors = (h, residual, gate, scale, post_weight, post_bias, weight, bias)
+        c = [None if t is None else t.detach().contiguous() for t in tensors]
+        r, y, kept = block_norm(*c, norm=norm, eps=eps, checkpoint=checkpoint)
+        if r is c[0]:
+            r = h.view_as(h)  # passed through: autograd wants an output of its own
+        ctx.norm, ctx.eps = norm, eps
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(*tensors)
+        return r, y, kept
+
+    @staticmethod
+    def backward(ctx, grad_r, grad_y, _):
+        tensors = ctx.saved_tensors
+        if grad_r is None and grad_y is None:
+            return (None,) * 11
+        c = [None if t is None else t.detach().contiguous() for t in tensors]
+        gr, gy = (None if g is None else g.to(c[0].dtype).contiguous() for g in (grad_r, grad_y))
+        need = (ctx.needs_input_grad + (False,) * 8)[:8]  # of the arguments that were given
+        return block_norm_backward(gr, gy, *c, norm=ctx.norm, eps=ctx.eps, need=need) + (None,) * 3

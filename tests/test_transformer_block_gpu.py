@@ -1,0 +1,142 @@
+"""The operators together, as a graph transformer's block uses them: norm with an
+8-bit checkpoint, transforms that keep it, attention over each graph with the
+learned bias, gate, residual scale and the next norm; forward and every gradient
+against the same block in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def pyg():
+    import paper_1903_02428_amd as m
+    assert torch.cuda.is_available()
+    m.library()
+    return m
+
+
+H, HKV, D, F, BUCKETS = 4, 2, 16, 64, 8
+LENGTHS = [30, 1, 55, 0, 90, 14]
+NAMES = ("x", "w_in", "b_in", "w_qkv", "table", "w_out", "w_gate", "scale", "post_w", "post_b", "w2", "b2")
+
+
+def params(seed=0):
+    g = torch.Generator().manual_seed(seed)
+    N = sum(LENGTHS)
+    shapes = {"x": (N, F), "w_in": (F,), "b_in": (F,), "w_qkv": (F, (H + 2 * HKV) * D), "table": (BUCKETS, H),
+              "w_out": (H * D, F), "w_gate": (F, F), "scale": (F,), "post_w": (F,), "post_b": (F,), "w2": (F,), "b2": (F,)}
+    p = {n: torch.randn(*s, generator=g) / (s[0] ** 0.5 if n.startswith("w_") and len(s) == 2 else 1) for n, s in shapes.items()}
+    return p, torch.randn(N, F, generator=g), torch.randn(N, F, generator=g)
+
+
+def block(pyg, p, ptr, lut):
+    _, y, kept = pyg.BlockNorm.apply(p["x"], None, None, None, None, None, p["w_in"], p["b_in"], "layer", 1e-5, True)
+    qkv = pyg.DenseTransform.apply(y, p["w_qkv"], kept).view(-1, H + 2 * HKV, D)
+    gate = pyg.DenseTransform.apply(y, p["w_gate"], kept)
+    o = pyg.GlobalAttention.apply(qkv[:, :H], qkv[:, H:H + HKV], qkv[:, H + HKV:], p["table"], ptr, None, lut)
+    h = pyg.DenseTransform.apply(o.reshape(-1, H * D), p["w_out"])
+    r, y2, _ = pyg.BlockNorm.apply(h, p["x"], gate, p["scale"], p["post_w"], p["post_b"], p["w2"], p["b2"])
+    return r, y2, y, o
+
+
+class _Kept(torch.autograd.Function):
+    """x W whose weight gradient takes the values that were kept in 8 bits."""
+
+    @staticmethod
+    def forward(ctx, x, w, kept):
+        ctx.save_for_backward(w, kept)
+        return x @ w
+
+    @staticmethod
+    def backward(ctx, g):
+        w, kept = ctx.saved_tensors
+        return g @ w.T, kept.T @ g, None
+
+
+def block64(p, lut, kept_y, kept_o):
+    def norm(x, w, b):
+        x = x - x.mean(1, keepdim=True)
+        return x / (x.square().mean(1, keepdim=True) + 1e-5).sqrt() * w + b
+    y = norm(p["x"], p["w_in"], p["b_in"])
+    qkv = _Kept.apply(y, p["w_qkv"], kept_y).view(-1, H + 2 * HKV, D)
+    gate = _Kept.apply(y, p["w_gate"], kept_y)
+    outs, at, R = [], 0, len(lut) // 2
+    for n in LENGTHS:
+        q, k, v = (t[at:at + n] for t in (qkv[:, :H], qkv[:, H:H + HKV], qkv[:, H + HKV:]))
+        k, v = k.repeat_interleave(H // HKV, 1), v.repeat_interleave(H // HKV, 1)
+        off = (torch.arange(n)[None] - torch.arange(n)[:, None]).clamp(-R, R) + R
+        a = torch.einsum("ihd,jhd->hij", q, k) * D ** -0.5 + p["table"][lut.long()[off]].permute(2, 0, 1)
+        outs.append(torch.einsum("hij,jhd->ihd", torch.softmax(a, 2), v))
+        at += n
+    h = _Kept.apply(torch.cat(outs).reshape(-1, H * D), p["w_out"], kept_o)
+    r = p["x"] + p["scale"] * torch.sigmoid(gate) * norm(h, p["post_w"], p["post_b"])
+    return r, norm(r, p["w2"], p["b2"])
+
+
+def run(pyg, p, gr, gy, ptr, lut):
+    dev = {n: t.cuda().requires_grad_(True) for n, t in p.items()}
+    r, y2, y, o = block(pyg, dev, ptr, lut)
+    grads = torch.autograd.grad([r, y2], [dev[n] for n in NAMES], [gr.cuda(), gy.cuda()])
+    return r, y2, dict(zip(NAMES, grads)), y.detach(), o.detach()
+
+
+def test_block(pyg):
+    p, gr, gy = params()
+    ptr = torch.tensor(np.concatenate([[0], np.cumsum(LENGTHS)]), dtype=torch.int64, device="cuda")
+    lut = pyg.relative_buckets(BUCKETS, 16)
+    r, y2, grads, y, o = run(pyg, p, gr, gy, ptr, lut)
+    kept_y, kept_o = (pyg.checkpoint_restore(pyg.activation_checkpoint(t)).cpu().double()
+                      for t in (y, o.reshape(-1, H * D)))
+    ref = {n: t.double().requires_grad_(True) for n, t in p.items()}
+    r64, y64 = block64(ref, lut.cpu(), kept_y, kept_o)
+    g64 = torch.autograd.grad([r64, y64], [ref[n] for n in NAMES], [gr.double(), gy.double()])
+    # seven stages, each off by at most a few hundred half steps of fp32 (sums of up to 190 terms) of its
+    # magnitudes, and magnitudes about three times the values: 7 * 300 * 3 * 2^-24 of the result's norm
+    tol = 7 * 300 * 3 * 2.0 ** -24
+    for name, got, want in [("r", r, r64), ("y", y2, y64)] + [(n, grads[n], g) for n, g in zip(NAMES, g64)]:
+        err = float((got.detach().cpu().double() - want.detach()).norm() / want.detach().norm())
+        assert err <= tol, f"{name}: {err:.3g}"
+    again = run(pyg, p, gr, gy, ptr, lut)
+    assert torch.equal(r, again[0]) and all(torch.equal(grads[n], again[2][n]) for n in NAMES)
+
+
+def test_two_streams_at_once(pyg):
+    """Two blocks at the same time on streams of their own give what each gives alone."""
+    ptr = torch.tensor(np.concatenate([[0], np.cumsum(LENGTHS)]), dtype=torch.int64, device="cuda")
+    lut = pyg.relative_buckets(BUCKETS, 16)
+    alone = [run(pyg, *params(s), ptr, lut) for s in (1, 2)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got[i] = run(pyg, *params(i + 1), ptr, lut)
+        torch.cuda.synchronize()
+        for a, b in zip(alone, got):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and all(torch.equal(a[2][n], b[2][n]) for n in NAMES)
+
+
+def test_captured_forward(pyg):
+    """A captured forward replays with other inputs, between eager work."""
+    p, _, _ = params(3)
+    dev = {n: t.cuda() for n, t in p.items()}
+    ptr = torch.tensor(np.concatenate([[0], np.cumsum(LENGTHS)]), dtype=torch.int64, device="cuda")
+    lut = pyg.relative_buckets(BUCKETS, 16)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        block(pyg, dev, ptr, lut)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        r, y2, _, _ = block(pyg, dev, ptr, lut)
+    for seed in (4, 5, 6):
+        dev["x"].copy_(params(seed)[0]["x"])
+        want = block(pyg, {n: t.clone() for n, t in dev.items()}, ptr, lut)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(r, want[0]) and torch.equal(y2, want[1])
