@@ -55,12 +55,18 @@ __device__ __forceinline__ void stage_bias(const Args &a, int h, float *bias) {
 // The other half's value of the same column (lanes l and l ^ 32).
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
+// A count or an offset in 32 bits: beyond 2^30 only its side matters.
+__device__ __forceinline__ int near(int64_t v) {
+    constexpr int64_t most = int64_t(1) << 30;
+    return static_cast<int>(v < -most ? -most : v > most ? most : v);
+}
+
 // Start of a 32 x 32 tile of scores whose lane holds column offset `col` and
 // rows 8 (r / 4) + 4 h + r % 4, offsets (key minus query) d0 + SIGN-ed index:
 // KEYS_IN_ROWS: rows are keys, the lane's column a query: d = d0 + row - m;
 // else rows are queries and the column a key: d = d0 + m - row.
 template <bool KEYS_IN_ROWS>
-__device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int64_t d0, int lane) {
+__device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int d0, int lane) {
     f32x16 c;
     // offsets of the tile: d0 - 31 .. d0 + 31
     if (d0 - 31 >= reach || d0 + 31 <= -reach) {
@@ -69,11 +75,11 @@ __device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int64_
         for (int r = 0; r < 16; ++r) c[r] = v;
         return c;
     }
-    const int m = lane & 31, h = lane >> 5, base = static_cast<int>(d0) + reach;
+    const int m = lane & 31, h = lane >> 5, base = d0 + reach + (KEYS_IN_ROWS ? 4 * h - m : m - 4 * h);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        const int row = 8 * (r >> 2) + 4 * h + (r & 3);
-        int o = base + (KEYS_IN_ROWS ? row - m : m - row);
+        const int row = 8 * (r >> 2) + (r & 3);
+        int o = KEYS_IN_ROWS ? base + row : base - row;
         o = o < 0 ? 0 : o > 2 * reach ? 2 * reach : o;
         c[r] = bias[o];
     }
@@ -83,7 +89,7 @@ __device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int64_
 // -infinity where there is no such key (rows from `keys` on) or it comes later
 // than the query (causal, offset > 0).
 template <bool KEYS_IN_ROWS>
-__device__ __forceinline__ void mask_tile(f32x16 &c, int64_t keys, int64_t queries, bool causal, int64_t d0, int lane) {
+__device__ __forceinline__ void mask_tile(f32x16 &c, int keys, int queries, bool causal, int d0, int lane) {
     if (keys >= 32 && queries >= 32 && (!causal || d0 + 31 <= 0)) return;
     const int m = lane & 31, h = lane >> 5;
 #pragma unroll

@@ -36,11 +36,13 @@ template <typename T>
 struct Elem;
 template <>
 struct Elem<__bf16> {
+    typedef uint16_t Bits;
     static constexpr int E = 8;      // values of a 16-byte piece
     static constexpr int kSteps = 2; // pieces of a contraction over 32 rows
 };
 template <>
 struct Elem<float> {
+    typedef uint32_t Bits;
     static constexpr int E = 4;
     static constexpr int kSteps = 4;
 };
@@ -85,77 +87,165 @@ __device__ __forceinline__ uint4 piece_of(const f32x16 &c, int u) {
     }
 }
 
-// Elements of one tile row in LDS: 16 bytes more than its DP features, so that
-// the 16-byte pieces of consecutive rows start four banks apart.
-template <typename T, int DP>
-constexpr int tile_stride() {
-    return DP + Elem<T>::E;
+// A tile of rows in LDS: rows of C chunks of 16 bytes, without padding (the
+// loads to LDS write 1 KB in a row), chunk c of a row at place c ^ swizzle(row). 16
+// consecutive rows then have any one chunk in 16 different groups of banks (row
+// pieces), and 4 rows times 4 chunks fill the 16 groups too (the transposing reads of
+// column pieces).
+template <int C>
+__device__ __forceinline__ int swizzle(int row) {
+    if constexpr (C == 4) return (row >> 2) & 3;
+    else if constexpr (C == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+    else return (row & 3) << 2 | ((row >> 2) & 3);
 }
 
-// Piece s of row `row` (contraction over the features).
 template <typename T, int DP>
-__device__ __forceinline__ uint4 row_piece(const T *tile, int row, int s, int h) {
-    constexpr int E = Elem<T>::E;
-    return *reinterpret_cast<const uint4 *>(tile + row * tile_stride<T, DP>() + 2 * E * s + E * h);
-}
+struct Tile {
+    static constexpr int E = Elem<T>::E, C = DP / E;
+    static constexpr int kRowBytes = DP * sizeof(T);
+    template <int ROWS>
+    static constexpr int bytes() { return ROWS * kRowBytes; }
 
-// Piece u of features d0 .. d0 + 31 of rows r0 .. r0 + 31 (contraction over the
-// rows): lane m holds feature d0 + m of the rows that piece_of's registers are.
-// bf16 goes through the transposing LDS read: lane i of 16 lanes names 8 bytes
-// (row i / 4 of 4, features 4 (i % 4) ..) and receives feature i of all four.
-template <typename T, int DP>
-__device__ __forceinline__ uint4 col_piece(const T *tile, int r0, int d0, int u, int lane) {
-    constexpr int S = tile_stride<T, DP>();
-    const int h = lane >> 5;
-    if constexpr (sizeof(T) == 2) {
-        const T *p = tile + (r0 + 16 * u + 4 * h + ((lane & 15) >> 2)) * S + d0 + (lane & 16) + 4 * (lane & 3);
-        typedef __attribute__((address_space(3))) short4v *lds4;
-        const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p)));
-        const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 8 * S)));
-        return make_uint4(a.x, a.y, b.x, b.y);
-    } else {
-        const T *p = tile + (r0 + 8 * u + 4 * h) * S + d0 + (lane & 31);
-        return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[S]), __float_as_uint(p[2 * S]),
-                          __float_as_uint(p[3 * S]));
+    // A lane's place for row pieces: row m of each 32, byte offset of piece s is at(s) + 32 n rows.
+    struct RowLane {
+        int base, x;
+        __device__ __forceinline__ explicit RowLane(int lane) {
+            const int m = lane & 31, h = lane >> 5;
+            base = m * kRowBytes, x = (h ^ swizzle<C>(m)) << 4;
+        }
+    };
+    static __device__ __forceinline__ uint4 row_piece(const char *tile, const RowLane &l, int n, int s) {
+        return *reinterpret_cast<const uint4 *>(tile + l.base + (l.x ^ (2 * s << 4)) + 32 * n * kRowBytes);
     }
-}
 
-// One 16-byte piece of a row in memory, from feature d on: zeros past D or
-// where `there` is false.
-template <typename T>
-__device__ __forceinline__ uint4 load_piece(const T *__restrict__ row, int d, int D, bool vec, bool there) {
-    constexpr int E = Elem<T>::E;
-    Piece<T> p;
-    p.u = make_uint4(0, 0, 0, 0);
-    if (!there || d >= D) return p.u;
-    if (vec) return *reinterpret_cast<const uint4 *>(row + d);
+    // A lane's place for column pieces. bf16 goes through the transposing LDS read:
+    // lane i of 16 lanes names 8 bytes (row i / 4 of 4, features 4 (i % 4) ..) and
+    // receives feature i of all four.
+    struct ColLane {
+        int base, x, lane;
+        __device__ __forceinline__ explicit ColLane(int lane_) : lane(lane_) {
+            const int h = lane >> 5;
+            if constexpr (sizeof(T) == 2) {
+                const int row = 4 * h + ((lane & 15) >> 2);
+                base = row * kRowBytes + (lane & 1) * 8;
+                x = (((lane & 16) >> 3 | (lane & 3) >> 1) ^ swizzle<C>(row)) << 4;
+            } else {
+                base = 4 * h * kRowBytes + (lane & 3) * 4;
+                x = ((lane & 31) >> 2 ^ h) << 4;  // swizzle of row 4 h + i + 8 u: h, and what i and u add
+            }
+        }
+    };
+    // Piece u of features 32 t .. of rows 32 n .. (contraction over the rows).
+    static __device__ __forceinline__ uint4 col_piece(const char *tile, const ColLane &l, int n, int t, int u) {
+        if constexpr (sizeof(T) == 2) {
+            const char *p = tile + l.base + (32 * n + 16 * u) * kRowBytes;
+            const int x = l.x ^ (t * 4 << 4);
+            typedef __attribute__((address_space(3))) short4v *lds4;
+            const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + x)));
+            const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 8 * kRowBytes + (x ^ 32))));
+            return make_uint4(a.x, a.y, b.x, b.y);
+        } else {
+            const char *p = tile + l.base + (32 * n + 8 * u) * kRowBytes;
+            uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-        if (d + i < D) p.v[i] = row[d + i];
-    return p.u;
-}
-
-// ROWS rows of a matrix, one head, held by a workgroup of NT threads between
-// memory and LDS.
-template <typename T, int DP, int ROWS, int NT>
-struct Stage {
-    static constexpr int E = Elem<T>::E, kRow = DP / E, kEach = (ROWS * kRow + NT - 1) / NT;
-    static_assert(ROWS * kRow % NT == 0, "whole pieces for every thread");
-    uint4 r[kEach];
-    // rows first .. first + ROWS of `base`, those from `end` on are zeros
-    __device__ __forceinline__ void load(const T *__restrict__ base, int64_t stride, int64_t first, int64_t end, int D,
-                                         bool vec) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int p = i * NT + threadIdx.x, row = p / kRow, d = p % kRow * E;
-            r[i] = load_piece<T>(base + (first + row) * stride, d, D, vec, first + row < end);
+            for (int i = 0; i < 4; ++i) {
+                const int add = swizzle<C>(i) ^ (u & 1) << 1 ^ t * 8;  // (row >> 2) & 3 = h + 2 (u & 1)
+                v[i] = *reinterpret_cast<const uint32_t *>(p + i * kRowBytes + (l.x ^ add << 4));
+            }
+            return make_uint4(v[0], v[1], v[2], v[3]);
         }
     }
-    __device__ __forceinline__ void store(T *tile) const {
+};
+
+// One 16-byte piece of a row in memory, from feature d on: zeros past D or
+// where `there` is false. Rows may start at any element (vector loads from memory
+// need no alignment here); the last piece of an odd width goes value by value.
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T *__restrict__ row, int d, int D, bool there) {
+    constexpr int E = Elem<T>::E;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef u32x4 __attribute__((aligned(2))) any;
+    if (there && d + E <= D) {
+        const u32x4 v = *reinterpret_cast<const any *>(row + d);
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    uint64_t lo = 0, hi = 0;
+    if (there) {
+        typedef typename Elem<T>::Bits Bits;
+#pragma unroll 1
+        for (int i = 0; d + i < D; ++i) {
+            const uint64_t b = static_cast<uint64_t>(reinterpret_cast<const Bits *>(row)[d + i]) << (8 * sizeof(T) * (i % (E / 2)));
+            (i < E / 2 ? lo : hi) |= b;
+        }
+    }
+    return make_uint4(static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi),
+                      static_cast<uint32_t>(hi >> 32));
+}
+
+// ROWS rows of one head, from memory to an LDS tile by a workgroup of NT
+// threads. 16-byte rows (vec) go without passing registers
+// (buffer_load_dwordx4 .. lds: 64 lanes write 1 KB in a row): the swizzle is in which
+// chunk a lane asks for, and rows past the end and features past D lie outside
+// the buffer, which reads as zeros. Other rows pass registers.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint32_t to_scalar(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint32_t lds_offset(const char *p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)(p)));
+}
+// 16 bytes a lane from the buffer's byte `off` to LDS bytes lds + 16 lane. In
+// assembly because the compiler, which cannot tell the halves of the LDS apart, makes
+// every LDS read wait for all such loads; loads_done() waits for them where it is
+// due, ahead of the barrier that hands the tile over.
+__device__ __forceinline__ void load_to_lds(const u32x4 &rsrc, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc)
+                 : "memory");
+}
+// (m0 is named nowhere else: these kernels index no register dynamically.)
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Ahead of a loop with such loads: the wavefront's own loads into registers arrive now, and the
+// compiler knows (vmcnt 0), or the loop's first use of one would wait in every round.
+__device__ __forceinline__ void registers_loaded() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    asm volatile("" ::: "memory");
+}
+
+constexpr uint32_t kOutside = 0x80000000u;
+constexpr int64_t kMaxRowStride = 1 << 22;  // in elements: 64 rows stay below kOutside
+
+template <typename T, int DP, int ROWS, int NT>
+struct Stage {
+    using L = Tile<T, DP>;
+    static constexpr int E = L::E, C = L::C, kEach = ROWS * C / NT;
+    static_assert(ROWS * C % NT == 0, "whole pieces for every thread");
+    uint32_t off[kEach];
+    uint32_t row_bytes;
+    int D;
+    bool vec;
+    __device__ __forceinline__ Stage(int64_t stride, int D_, bool vec_) : row_bytes(stride * sizeof(T)), D(D_), vec(vec_) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int p = i * NT + threadIdx.x, row = p / kRow, d = p % kRow * E;
-            *reinterpret_cast<uint4 *>(tile + row * tile_stride<T, DP>() + d) = r[i];
+            const int p = i * NT + threadIdx.x, row = p / C, d = ((p % C) ^ swizzle<C>(row)) * E;
+            off[i] = d < D ? row * row_bytes + d * sizeof(T) : kOutside;
+        }
+    }
+    // rows first .. of `head` (a [rows] array of this head's features); there are `left` of them
+    __device__ __forceinline__ void load(const T *head, int64_t first, int64_t left, char *tile) const {
+        const T *base = head + first * (row_bytes / sizeof(T));
+        const int rows = left < ROWS ? static_cast<int>(left) : ROWS;
+        if (vec) {
+            const uint64_t at = reinterpret_cast<uint64_t>(base);
+            const u32x4 rsrc{to_scalar(static_cast<uint32_t>(at)), to_scalar(static_cast<uint32_t>(at >> 32) & 0xFFFFu),
+                             to_scalar(rows * row_bytes), 0x00020000u};
+            const uint32_t wave = to_scalar(lds_offset(tile) + (threadIdx.x >> 6) * 1024u);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) load_to_lds(rsrc, off[i], wave + i * NT * 16u);
+        } else {
+#pragma unroll 1
+            for (int p = threadIdx.x; p < ROWS * C; p += NT) {
+                const int row = p / C, d = ((p % C) ^ swizzle<C>(row)) * E;
+                *reinterpret_cast<uint4 *>(tile + p * 16) =
+                    load_piece<T>(base + (int64_t)row * (row_bytes / sizeof(T)), d, D, row < rows);
+            }
         }
     }
 };

@@ -16,7 +16,7 @@ using attn::f32x16;
 
 // One thread a piece of 16 bytes of x: E lanes' neighbours share a block of 32.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_checkpoint(const T *__restrict__ x, int64_t N, int F, int pieces, bool vec,
+__global__ __launch_bounds__(kBlock) void k_checkpoint(const T *__restrict__ x, int64_t N, int F, int pieces,
                                                        uint8_t *__restrict__ codes, uint8_t *__restrict__ steps) {
     constexpr int E = 16 / sizeof(T);
     const int64_t all = N * pieces, step = (int64_t)gridDim.x * kBlock;
@@ -24,7 +24,7 @@ __global__ __launch_bounds__(kBlock) void k_checkpoint(const T *__restrict__ x, 
         const int64_t row = i / pieces;                                                 // blocks stay in 8 or 4 lanes
         const int f = static_cast<int>(i - row * pieces) * E;
         attn::Piece<T> p;
-        p.u = attn::load_piece<T>(x + row * F, f, F, vec, true);
+        p.u = attn::load_piece<T>(x + row * F, f, F, true);
         float v[E];
         uint32_t top = 0;
 #pragma unroll
@@ -85,23 +85,24 @@ __global__ __launch_bounds__(kBlock) void k_restore(const uint8_t *__restrict__ 
 
 constexpr int kTileI = 128, kTileO = 128, kTileN = 32;
 typedef __bf16 bf16;
-constexpr int kStride = attn::tile_stride<bf16, 128>();
+using Rows = attn::Tile<bf16, 128>;
 
 // A workgroup owns 128 x 128 of dTheta and every splits-th tile of 32 rows. PARTS
 // bf16 parts of G (1: bf16 G, 3: fp32 G).
 template <typename T, int PARTS>
 __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ steps,
                                                        const T *__restrict__ g, int64_t N, int Fi, int Fo, int blocks,
-                                                       bool vec, int splits, float *__restrict__ part) {
+                                                       int splits, float *__restrict__ part) {
     constexpr int E = 16 / sizeof(T), GP = kTileN * kTileO / E / kBlock;
-    __shared__ __align__(16) bf16 xt[kTileN * kStride];
-    __shared__ __align__(16) bf16 gt[PARTS][kTileN * kStride];
+    __shared__ __align__(16) char xt[Rows::bytes<kTileN>()];
+    __shared__ __align__(16) char gt[PARTS][Rows::bytes<kTileN>()];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int tiles_o = (Fo + kTileO - 1) / kTileO;
     const int sp = blockIdx.x % splits, tile = blockIdx.x / splits;
     const int i0 = tile / tiles_o * kTileI, o0 = tile % tiles_o * kTileO;
     const int wi = wave / 2 * 64, wo = wave % 2 * 64;  // the wavefront's 64 x 64
     const int64_t width = (int64_t)blocks * 32;
+    const Rows::ColLane cl(lane);
     f32x16 acc[2][2];
 #pragma unroll
     for (int a = 0; a < 2; ++a)
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
             const int p = j * kBlock + threadIdx.x, r = p / (kTileO / E), c = p % (kTileO / E) * E;
-            cg[j] = attn::load_piece<T>(g + (n0 + r) * Fo, o0 + c, Fo, vec, n0 + r < N);
+            cg[j] = attn::load_piece<T>(g + (n0 + r) * Fo, o0 + c, Fo, n0 + r < N);
         }
     };
     auto store = [&]() {
@@ -136,13 +137,15 @@ __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict
             eight::unpack(w[j], v);
             o[2 * j] = attn::pack_bf16(v[0] * s, v[1] * s), o[2 * j + 1] = attn::pack_bf16(v[2] * s, v[3] * s);  // exact
         }
-        uint4 *x = reinterpret_cast<uint4 *>(xt + xr * kStride + xc);
-        x[0] = make_uint4(o[0], o[1], o[2], o[3]), x[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        char *x = xt + xr * Rows::kRowBytes;
+        const int sw = attn::swizzle<Rows::C>(xr);
+        *reinterpret_cast<uint4 *>(x + ((xc / 8 ^ sw) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4 *>(x + ((xc / 8 + 1 ^ sw) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
             const int p = j * kBlock + threadIdx.x, r = p / (kTileO / E), c = p % (kTileO / E) * E;
             if constexpr (PARTS == 1) {
-                *reinterpret_cast<uint4 *>(gt[0] + r * kStride + c) = cg[j];
+                *reinterpret_cast<uint4 *>(gt[0] + r * Rows::kRowBytes + ((c / 8 ^ attn::swizzle<Rows::C>(r)) << 4)) = cg[j];
             } else {
                 attn::Piece<T> v;
                 v.u = cg[j];
@@ -156,7 +159,8 @@ __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict
                         // an infinity or NaN is all in the first part
                         f[e] = (b[e] & 0x7F800000u) == 0x7F800000u ? 0.f : f[e] - __uint_as_float(b[e]);
                     }
-                    *reinterpret_cast<uint2 *>(gt[k] + r * kStride + c) = make_uint2(b[0] >> 16 | b[1], b[2] >> 16 | b[3]);
+                    *reinterpret_cast<uint2 *>(gt[k] + r * Rows::kRowBytes + ((c / 8 ^ attn::swizzle<Rows::C>(r)) << 4) + c % 8 * 2) =
+                        make_uint2(b[0] >> 16 | b[1], b[2] >> 16 | b[3]);
                 }
             }
         }
@@ -172,12 +176,12 @@ __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict
         for (int u = 0; u < 2; ++u) {
             uint4 a[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) a[t] = attn::col_piece<bf16, 128>(xt, 0, wi + 32 * t, u, lane);
+            for (int t = 0; t < 2; ++t) a[t] = Rows::col_piece(xt, cl, 0, wi / 32 + t, u);
 #pragma unroll
             for (int k = PARTS - 1; k >= 0; --k)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const uint4 y = attn::col_piece<bf16, 128>(gt[k], 0, wo + 32 * b, u, lane);
+                    const uint4 y = Rows::col_piece(gt[k], cl, 0, wo / 32 + b, u);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) acc[t][b] = attn::mma<bf16>(a[t], y, acc[t][b]);
                 }
@@ -244,7 +248,7 @@ int theta_grad(const T *g, int64_t N, int Fo, int Fi, const int8_t *codes, const
     const int64_t tiles = ((int64_t)(Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO), n = (int64_t)Fi * Fo;
     if (tiles * splits * kBlock >= (int64_t(1) << 32) || n / 32 * kBlock >= (int64_t(1) << 32)) return PYG_ERR_UNSUPPORTED;
     k_theta_grad<T, sizeof(T) == 2 ? 1 : 3><<<static_cast<unsigned>(tiles * splits), kBlock, 0, s>>>(
-        reinterpret_cast<const uint8_t *>(codes), steps, g, N, Fi, Fo, blocks, aligned(g, (int64_t)Fo * sizeof(T)), splits, part);
+        reinterpret_cast<const uint8_t *>(codes), steps, g, N, Fi, Fo, blocks, splits, part);
     PYG_LAUNCH_CHECK();
     k_join_theta<T><<<static_cast<unsigned>((n + 31) / 32), kBlock, 0, s>>>(part, n, splits, out);
     PYG_LAUNCH_CHECK();
@@ -267,9 +271,9 @@ extern "C" int pyg_activation_checkpoint(const void *x, int dtype, int64_t N, in
     uint8_t *c = reinterpret_cast<uint8_t *>(codes);
     const unsigned grid = grid_for(N * (width / (dtype == PYG_BF16 ? 8 : 4)), kBlock, 1 << 16);
     if (dtype == PYG_BF16)
-        k_checkpoint<__bf16><<<grid, kBlock, 0, s>>>(static_cast<const __bf16 *>(x), N, f, width / 8, aligned(x, F * 2), c, steps);
+        k_checkpoint<__bf16><<<grid, kBlock, 0, s>>>(static_cast<const __bf16 *>(x), N, f, width / 8, c, steps);
     else
-        k_checkpoint<float><<<grid, kBlock, 0, s>>>(static_cast<const float *>(x), N, f, width / 4, aligned(x, F * 4), c, steps);
+        k_checkpoint<float><<<grid, kBlock, 0, s>>>(static_cast<const float *>(x), N, f, width / 4, c, steps);
     PYG_LAUNCH_CHECK();
     return PYG_OK;
 }

@@ -6,21 +6,25 @@ namespace pyg {
 namespace attn {
 namespace {
 
+// Wavefronts a SIMD that the registers have to leave room for.
+template <typename T, int DP, int WAVES>
+constexpr int kForwardWaves = DP <= 64 ? 2 : sizeof(T) == 2 ? 2 : 1;
+
 // A workgroup owns 32 * WAVES queries of one graph and head and walks over the
 // graph's keys in tiles of BK, staged in LDS for its wavefronts; a wavefront
 // keeps 32 queries. S^T = K Q^T puts a query in a lane's column, so the running
 // maximum and sum are one value a lane and P^T is the second product's operand
 // as it stands: O^T = V^T P^T.
 template <typename T, int DP, int WAVES, int BK>
-__global__ __launch_bounds__(64 * WAVES) void k_forward(const Args a, int64_t nslots) {
+__global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_forward(const Args a, int64_t nslots) {
     constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
-    constexpr int stride = tile_stride<T, DP>();
-    extern __shared__ __align__(16) char lds[];
-    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BK * stride;
-    float *bias = reinterpret_cast<float *>(vt + BK * stride);
+    using L = Tile<T, DP>;
+    constexpr int kTile = L::template bytes<BK>();
+    extern __shared__ __align__(16) char lds[];  // K and V of two tiles, the bias
+    float *bias = reinterpret_cast<float *>(lds + 4 * kTile);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
     // key heads vary fastest: with up to 8 of them (or a multiple) every XCD's L2 sees its own heads' keys only
-    const int64_t id = blockIdx.x;
+    const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
     const int64_t slot = nslots - 1 - id / a.H;  // causal: the longest walks first
     const Place pq = place_of(a.q_ptr, a.B, a.Nq, slot, BM, 1, lane);
@@ -35,15 +39,18 @@ __global__ __launch_bounds__(64 * WAVES) void k_forward(const Args a, int64_t ns
     const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
                   k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
     const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
-    const T *kb = static_cast<const T *>(a.k) + hk * a.k_head, *vb = static_cast<const T *>(a.v) + hk * a.v_head;
+    const T *kb = static_cast<const T *>(a.k) + hk * a.k_head + k_first * a.k_row;
+    const T *vb = static_cast<const T *>(a.v) + hk * a.v_head + k_first * a.v_row;
 
-    const int64_t i0 = pq.tile * BM + wave * 32;           // first query of the wavefront, in the graph
-    const int64_t row = pq.first + i0 + m;                 // the lane's query row
+    const int64_t i0 = pq.tile * BM + wave * 32;  // first query of the wavefront, in the graph
+    const int64_t row = pq.first + i0 + m;        // the lane's query row
     const bool there = row < pq.last;
     uint4 qf[SQ];
-    const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
+    {
+        const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
 #pragma unroll
-    for (int s = 0; s < SQ; ++s) qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, a.vec_q, there);
+        for (int s = 0; s < SQ; ++s) qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, there);
+    }
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -55,29 +62,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_forward(const Args a, int64_t ns
         const int64_t seen = pq.tile * BM + BM + nk - nq;  // keys that the last query of the workgroup may see
         end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
     }
-    Stage<T, DP, BK, NT> sk, sv;
-    if (end > 0) {
-        sk.load(kb, a.k_row, k_first, k_last, a.D, a.vec_k);
-        sv.load(vb, a.v_row, k_first, k_last, a.D, a.vec_v);
-    }
-    for (int64_t j0 = 0; j0 < end; j0 += BK) {
-        __syncthreads();
-        sk.store(kt);
-        sv.store(vt);
-        __syncthreads();
-        if (j0 + BK < end) {
-            sk.load(kb, a.k_row, k_first + j0 + BK, k_last, a.D, a.vec_k);
-            sv.load(vb, a.v_row, k_first + j0 + BK, k_last, a.D, a.vec_v);
-        }
-        const int64_t d0 = j0 - (i0 + nk - nq);  // offset of the tile's first key and the wavefront's first query
-        if (a.causal && d0 > 31) continue;       // later than all of the wavefront's queries
+    const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
+    const typename L::RowLane rl(lane);
+    const typename L::ColLane cl(lane);
+    const int64_t shift = i0 + nk - nq;  // offset of key j and the wavefront's first query: j - shift
+    auto step = [&](const char *kt, const char *vt, int64_t j0) {
+        const int d0 = near(j0 - shift), left = near(nk - j0);
+        if (a.causal && d0 > 31) return;  // later than all of the wavefront's queries
         f32x16 st[NK];
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
             st[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
 #pragma unroll
-            for (int s = 0; s < SQ; ++s) st[n] = mma<T>(row_piece<T, DP>(kt, 32 * n + m, s, h), qf[s], st[n]);
-            mask_tile<true>(st[n], nk - j0 - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+            for (int s = 0; s < SQ; ++s) st[n] = mma<T>(L::row_piece(kt, rl, n, s), qf[s], st[n]);
+            mask_tile<true>(st[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
         }
         float t = kNegInf;
 #pragma unroll
@@ -115,9 +113,28 @@ __global__ __launch_bounds__(64 * WAVES) void k_forward(const Args a, int64_t ns
                 // summand, no more than the result's own rounding; the sum of P keeps 32 bits
                 const uint4 p = piece_of<T>(st[n], u);
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) acc[d] = mma<T>(col_piece<T, DP>(vt, 32 * n, 32 * d, u, lane), p, acc[d]);
+                for (int d = 0; d < DP / 32; ++d) acc[d] = mma<T>(L::col_piece(vt, cl, n, d, u), p, acc[d]);
             }
         }
+    };
+    // the next tile is on its way to one half of the LDS while the other is worked on
+    auto fetch = [&](int64_t j0, int half) {
+        if (j0 >= end) return;
+        sk.load(kb, j0, nk - j0, lds + 2 * half * kTile);
+        sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
+    };
+    registers_loaded();
+    fetch(0, 0);
+    for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
+        loads_done();
+        __syncthreads();  // the tile is there, and nobody reads the other half any more
+        fetch(j0 + BK, 1);
+        step(lds, lds + kTile, j0);
+        if (j0 + BK >= end) break;
+        loads_done();
+        __syncthreads();
+        fetch(j0 + 2 * BK, 0);
+        step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
     }
     sum += other_half(sum);
     store_rows<T, DP>(out, row, there, a.H, head, a.D, a.vec_o, acc, top == kNegInf ? 0.f : 1.f / sum, lane);
@@ -128,7 +145,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_forward(const Args a, int64_t ns
 template <typename T, int DP, int WAVES, int BK>
 int launch(const Args &a, hipStream_t s) {
     const int64_t n = slots(a.Nq, a.B, 32 * WAVES);
-    const size_t bytes = 2 * BK * tile_stride<T, DP>() * sizeof(T) + (2 * a.reach + 1) * sizeof(float);
+    const size_t bytes = 4 * Tile<T, DP>::template bytes<BK>() + (2 * a.reach + 1) * sizeof(float);
     if (n * a.H >= (int64_t(1) << 32) / (64 * WAVES)) return PYG_ERR_UNSUPPORTED;
     k_forward<T, DP, WAVES, BK><<<static_cast<unsigned>(n * a.H), 64 * WAVES, bytes, s>>>(a, n);
     PYG_LAUNCH_CHECK();
@@ -138,7 +155,7 @@ int launch(const Args &a, hipStream_t s) {
 template <typename T, int DP>
 int by_waves(const Args &a, hipStream_t s) {
     if (a.Nq <= 64 * a.B) return launch<T, DP, 1, 32>(a, s);
-    return launch<T, DP, 4, 64>(a, s);
+    return launch<T, DP, 4, DP * sizeof(T) <= 256 ? 64 : 32>(a, s);
 }
 
 template <typename T>
@@ -206,11 +223,14 @@ int take_inputs(const pyg_attention *c, const void *q, const void *k, const void
     if (!strided(c->q_row, c->q_head, c->Nq, c->H, c->D) || !strided(c->k_row, c->k_head, c->Nk, c->Hkv, c->D) ||
         !strided(c->v_row, c->v_head, c->Nk, c->Hkv, c->D))
         return PYG_ERR_INVALID_ARG;
+    if (c->q_row >= kMaxRowStride || c->k_row >= kMaxRowStride || c->v_row >= kMaxRowStride) return PYG_ERR_UNSUPPORTED;
+    if (c->Nq <= 1) a->q_row = c->D;  // a single row's stride says nothing
+    if (c->Nk <= 1) a->k_row = a->v_row = c->D;
     const size_t e = bytes_of(c);
     a->q = q, a->k = k, a->v = v;
-    a->vec_q = vectors(q, c->q_row, c->q_head, c->D, e);
-    a->vec_k = vectors(k, c->k_row, c->k_head, c->D, e);
-    a->vec_v = vectors(v, c->v_row, c->v_head, c->D, e);
+    a->vec_q = vectors(q, a->q_row, c->q_head, c->D, e);
+    a->vec_k = vectors(k, a->k_row, c->k_head, c->D, e);
+    a->vec_v = vectors(v, a->v_row, c->v_head, c->D, e);
     return PYG_OK;
 }
 

@@ -17,25 +17,27 @@ namespace {
 struct RowStat {
     float top, log_sum, lse;  // lse = c2 top + log2 sum, infinite for a row that sees no key
 };
-__device__ __forceinline__ RowStat row_stat(const float *__restrict__ stat, int64_t at, float c2) {
-    const float2 s = *reinterpret_cast<const float2 *>(stat + 2 * at);
+__device__ __forceinline__ RowStat row_stat(float2 s, float c2) {
     return {s.x, s.y, s.x == kNegInf ? -kNegInf : fmaf(c2, s.x, s.y)};
 }
-constexpr RowStat kNoRow{kNegInf, 0.f, -kNegInf};
+
+// Wavefronts a SIMD that the registers have to leave room for.
+template <typename T, int DP>
+constexpr int kGradWaves = DP <= 64 ? 2 : 1;
 
 // A workgroup owns 32 * WAVES queries, as in the forward.
 template <typename T, int DP, int WAVES, int BK>
-__global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int64_t nslots, float *__restrict__ delta,
+__global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(const BackwardArgs b, int64_t nslots, float *__restrict__ delta,
                                                        float *__restrict__ part) {
     const Args &a = b.f;
     constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
-    constexpr int stride = tile_stride<T, DP>();
-    extern __shared__ __align__(16) char lds[];
-    T *kt = reinterpret_cast<T *>(lds), *vt = kt + BK * stride;
-    float *bias = reinterpret_cast<float *>(vt + BK * stride);
+    using L = Tile<T, DP>;
+    constexpr int kTile = L::template bytes<BK>();
+    extern __shared__ __align__(16) char lds[];  // K and V of two tiles, the bias, the sums by offset
+    float *bias = reinterpret_cast<float *>(lds + 4 * kTile);
     float *hist = bias + (2 * a.reach + 1);  // a wavefront's own sums by offset
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
-    const int64_t id = blockIdx.x;
+    const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
     const int64_t slot = nslots - 1 - id / a.H;
     float *mine = part ? part + (slot * a.H + head) * a.buckets : nullptr;  // the workgroup's share of dT
@@ -56,7 +58,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int
     const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
                   k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
     const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
-    const T *kb = static_cast<const T *>(a.k) + hk * a.k_head, *vb = static_cast<const T *>(a.v) + hk * a.v_head;
+    const T *kb = static_cast<const T *>(a.k) + hk * a.k_head + k_first * a.k_row;
+    const T *vb = static_cast<const T *>(a.v) + hk * a.v_head + k_first * a.v_row;
 
     const int64_t i0 = pq.tile * BM + wave * 32, row = pq.first + i0 + m;
     const bool there = row < pq.last;
@@ -67,19 +70,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int
     float dl = 0.f;
 #pragma unroll
     for (int s = 0; s < SQ; ++s) {
-        qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, a.vec_q, there);
+        qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, there);
         Piece<T> g, o;
-        g.u = gf[s] = load_piece<T>(gr, 2 * E * s + E * h, a.D, a.vec_o, there);
-        o.u = load_piece<T>(orow, 2 * E * s + E * h, a.D, a.vec_o, there);
+        g.u = gf[s] = load_piece<T>(gr, 2 * E * s + E * h, a.D, there);
+        o.u = load_piece<T>(orow, 2 * E * s + E * h, a.D, there);
 #pragma unroll
         for (int i = 0; i < E; ++i) dl = fmaf(to_f32(g.v[i]), to_f32(o.v[i]), dl);
     }
     dl += other_half(dl);
-    RowStat st = kNoRow;
+    float2 raw = make_float2(kNegInf, 0.f);
     if (there) {
-        st = row_stat(a.stat, row * a.H + head, a.c2);
+        raw = *reinterpret_cast<const float2 *>(a.stat + (row * a.H + head) * 2);
         if (h == 0) delta[row * a.H + head] = dl;
     }
+    const RowStat st = row_stat(raw, a.c2);
     const bool wild = __any(st.top != kNegInf && fabsf(st.top) > kWild);
 
     f32x16 acc[DP / 32];
@@ -92,31 +96,22 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int
         const int64_t seen = pq.tile * BM + BM + nk - nq;
         end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
     }
-    Stage<T, DP, BK, NT> sk, sv;
-    if (end > 0) {
-        sk.load(kb, a.k_row, k_first, k_last, a.D, a.vec_k);
-        sv.load(vb, a.v_row, k_first, k_last, a.D, a.vec_v);
-    }
-    for (int64_t j0 = 0; j0 < end; j0 += BK) {
-        __syncthreads();
-        sk.store(kt);
-        sv.store(vt);
-        __syncthreads();
-        if (j0 + BK < end) {
-            sk.load(kb, a.k_row, k_first + j0 + BK, k_last, a.D, a.vec_k);
-            sv.load(vb, a.v_row, k_first + j0 + BK, k_last, a.D, a.vec_v);
-        }
+    const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
+    const typename L::RowLane rl(lane);
+    const typename L::ColLane cl(lane);
+    const int64_t shift = i0 + nk - nq;
+    auto step = [&](const char *kt, const char *vt, int64_t j0) {
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-            const int64_t d0 = j0 + 32 * n - (i0 + nk - nq);
-            if ((a.causal && d0 > 31) || j0 + 32 * n >= nk) continue;
+            const int d0 = near(j0 + 32 * n - shift), left = near(nk - j0 - 32 * n);
+            if ((a.causal && d0 > 31) || left <= 0) continue;
             f32x16 s = bias_tile<true>(bias, a.reach, d0, lane), dp = f32x16(0.f);
 #pragma unroll
             for (int u = 0; u < SQ; ++u) {
-                s = mma<T>(row_piece<T, DP>(kt, 32 * n + m, u, h), qf[u], s);
-                dp = mma<T>(row_piece<T, DP>(vt, 32 * n + m, u, h), gf[u], dp);
+                s = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s);
+                dp = mma<T>(L::row_piece(vt, rl, n, u), gf[u], dp);
             }
-            mask_tile<true>(s, nk - j0 - 32 * n, 32, a.causal, d0, lane);
+            mask_tile<true>(s, left, 32, a.causal, d0, lane);
             if (wild) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -135,7 +130,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int
                     (d0 > 0 ? above : below) += t;
                 } else {
                     // at most two lanes of an instruction meet in an offset: their column and row differ alike
-                    const int base = static_cast<int>(d0) + a.reach - m + 4 * h;
+                    const int base = d0 + a.reach - m + 4 * h;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         int o = base + 8 * (r >> 2) + (r & 3);
@@ -148,9 +143,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int
             for (int u = 0; u < Elem<T>::kSteps; ++u) {
                 const uint4 p = piece_of<T>(s, u);  // dS rounded once to the operands' type
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) acc[t] = mma<T>(col_piece<T, DP>(kt, 32 * n, 32 * t, u, lane), p, acc[t]);
+                for (int t = 0; t < DP / 32; ++t) acc[t] = mma<T>(L::col_piece(kt, cl, n, t, u), p, acc[t]);
             }
         }
+    };
+    auto fetch = [&](int64_t j0, int half) {
+        if (j0 >= end) return;
+        sk.load(kb, j0, nk - j0, lds + 2 * half * kTile);
+        sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
+    };
+    registers_loaded();
+    fetch(0, 0);
+    for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
+        loads_done();
+        __syncthreads();
+        fetch(j0 + BK, 1);
+        step(lds, lds + kTile, j0);
+        if (j0 + BK >= end) break;
+        loads_done();
+        __syncthreads();
+        fetch(j0 + 2 * BK, 0);
+        step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
     }
     store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
     if (mine) {
@@ -175,17 +188,18 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_q(const BackwardArgs b, int
 // key in a lane's column: P and dS are the operands of dV^T = g^T P and
 // dK^T = Q^T dS as they stand.
 template <typename T, int DP, int WAVES, int BQ>
-__global__ __launch_bounds__(64 * WAVES) void k_grad_kv(const BackwardArgs b, int64_t nslots,
+__global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(const BackwardArgs b, int64_t nslots,
                                                         const float *__restrict__ delta) {
     const Args &a = b.f;
     constexpr int NT = 64 * WAVES, BN = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NQ = BQ / 32;
-    constexpr int stride = tile_stride<T, DP>();
-    extern __shared__ __align__(16) char lds[];
-    T *qt = reinterpret_cast<T *>(lds), *gt = qt + BQ * stride;
-    float *stats = reinterpret_cast<float *>(gt + BQ * stride);  // [BQ] each: lse, top, delta, log2 sum
-    float *bias = stats + 4 * BQ;
+    using L = Tile<T, DP>;
+    constexpr int kTile = L::template bytes<BQ>();
+    static_assert(BQ <= NT, "a thread a query's statistics");
+    extern __shared__ __align__(16) char lds[];  // Q and dO of two tiles, their statistics, the bias
+    float *stats = reinterpret_cast<float *>(lds + 4 * kTile);  // [2][4][BQ]: lse, top, delta, log2 sum
+    float *bias = stats + 8 * BQ;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
-    const int64_t id = blockIdx.x;
+    const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv;
     const int64_t slot = id / a.Hkv;  // causal: the first keys are seen by the most queries
     const Place pk = place_of(a.k_ptr, a.B, a.Nk, slot, BN, 1, lane);
@@ -207,9 +221,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_kv(const BackwardArgs b, in
     const T *vr = static_cast<const T *>(a.v) + row * a.v_row + hk * a.v_head;
 #pragma unroll
     for (int s = 0; s < SQ; ++s) {
-        kf[s] = load_piece<T>(kr, 2 * E * s + E * h, a.D, a.vec_k, there);
-        vf[s] = load_piece<T>(vr, 2 * E * s + E * h, a.D, a.vec_v, there);
+        kf[s] = load_piece<T>(kr, 2 * E * s + E * h, a.D, there);
+        vf[s] = load_piece<T>(vr, 2 * E * s + E * h, a.D, there);
     }
+    const int keys = near(nk - j0);
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = f32x16(0.f);
@@ -219,70 +234,62 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_kv(const BackwardArgs b, in
         begin = pk.tile * BN - (nk - nq);
         begin = begin < 0 ? 0 : begin / 32 * 32;
     }
-    for (int g = 0; g < a.G; ++g) {
+    const Stage<T, DP, BQ, NT> sq(a.q_row, a.D, a.vec_q), sg((int64_t)a.H * a.D, a.D, a.vec_o);
+    const typename L::RowLane rl(lane);
+    const typename L::ColLane cl(lane);
+    for (int g = 0; g < a.G && begin < nq; ++g) {
         const int head = hk * a.G + g;
-        __syncthreads();
-        stage_bias<T>(a, head, bias);
-        const T *qb = static_cast<const T *>(a.q) + head * a.q_head;
-        const T *gb = static_cast<const T *>(b.grad_out) + (int64_t)head * a.D;
-        const int64_t g_row = (int64_t)a.H * a.D;
-        Stage<T, DP, BQ, NT> sq, sg;
-        if (begin < nq) {
-            sq.load(qb, a.q_row, q_first + begin, q_last, a.D, a.vec_q);
-            sg.load(gb, g_row, q_first + begin, q_last, a.D, a.vec_o);
-        }
-        for (int64_t i0 = begin; i0 < nq; i0 += BQ) {
-            __syncthreads();
-            sq.store(qt);
-            sg.store(gt);
-            for (int i = threadIdx.x; i < BQ; i += NT) {
-                const int64_t r = q_first + i0 + i;
-                RowStat st = kNoRow;
-                float dl = 0.f;
-                if (r < q_last) {
-                    st = row_stat(a.stat, r * a.H + head, a.c2);
-                    dl = delta[r * a.H + head];
-                }
-                stats[i] = st.lse, stats[BQ + i] = st.top, stats[2 * BQ + i] = dl, stats[3 * BQ + i] = st.log_sum;
+        const T *qb = static_cast<const T *>(a.q) + head * a.q_head + q_first * a.q_row;
+        const T *gb = static_cast<const T *>(b.grad_out) + (q_first * a.H + head) * a.D;
+        float2 next = make_float2(kNegInf, 0.f);
+        float next_delta = 0.f;
+        // Q and dO of the next tile go to the other half of the LDS, its statistics by way of registers
+        auto fetch = [&](int64_t i0, int half) {
+            if (i0 >= nq) return;
+            sq.load(qb, i0, nq - i0, lds + 2 * half * kTile);
+            sg.load(gb, i0, nq - i0, lds + (2 * half + 1) * kTile);
+            const int64_t r = i0 + threadIdx.x;
+            next = make_float2(kNegInf, 0.f), next_delta = 0.f;
+            if (threadIdx.x < BQ && r < nq) {
+                next = *reinterpret_cast<const float2 *>(a.stat + ((q_first + r) * a.H + head) * 2);
+                next_delta = delta[(q_first + r) * a.H + head];
             }
-            __syncthreads();
-            if (i0 + BQ < nq) {
-                sq.load(qb, a.q_row, q_first + i0 + BQ, q_last, a.D, a.vec_q);
-                sg.load(gb, g_row, q_first + i0 + BQ, q_last, a.D, a.vec_o);
+        };
+        auto put = [&](int half) {
+            if (threadIdx.x < BQ) {
+                const RowStat t = row_stat(next, a.c2);
+                float *s = stats + half * 4 * BQ + threadIdx.x;
+                s[0] = t.lse, s[BQ] = t.top, s[2 * BQ] = next_delta, s[3 * BQ] = t.log_sum;
             }
+        };
+        auto step = [&](const char *qt, const char *gt, const float *stat, int64_t i0) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                const int64_t d0 = j0 - (i0 + 32 * n + nk - nq);
-                if ((a.causal && d0 > 31) || i0 + 32 * n >= nq) continue;
+                const int d0 = near(j0 - (i0 + 32 * n + nk - nq)), left = near(nq - i0 - 32 * n);
+                if ((a.causal && d0 > 31) || left <= 0) continue;
                 f32x16 s = bias_tile<false>(bias, a.reach, d0, lane), dp = f32x16(0.f);
 #pragma unroll
                 for (int u = 0; u < SQ; ++u) {
-                    s = mma<T>(row_piece<T, DP>(qt, 32 * n + m, u, h), kf[u], s);
-                    dp = mma<T>(row_piece<T, DP>(gt, 32 * n + m, u, h), vf[u], dp);
+                    s = mma<T>(L::row_piece(qt, rl, n, u), kf[u], s);
+                    dp = mma<T>(L::row_piece(gt, rl, n, u), vf[u], dp);
                 }
-                mask_tile<false>(s, nk - j0, nq - i0 - 32 * n, a.causal, d0, lane);
-                bool wild = false;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 t = *reinterpret_cast<const float4 *>(stats + BQ + 32 * n + 8 * q + 4 * h);
-                    const float v[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) wild |= v[i] != kNegInf && fabsf(v[i]) > kWild;
-                }
-                wild = __any(wild);
+                mask_tile<false>(s, keys, left, a.causal, d0, lane);
+                const float *tops = stat + BQ + 32 * n;
+                const float my_top = tops[m];
+                const bool wild = __any(my_top != kNegInf && fabsf(my_top) > kWild);
                 f32x16 ds;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int at = 32 * n + 8 * q + 4 * h;
-                    const float4 l = *reinterpret_cast<const float4 *>(stats + at);
-                    const float4 e = *reinterpret_cast<const float4 *>(stats + 2 * BQ + at);
+                    const float4 l = *reinterpret_cast<const float4 *>(stat + at);
+                    const float4 e = *reinterpret_cast<const float4 *>(stat + 2 * BQ + at);
                     const float ls[4] = {l.x, l.y, l.z, l.w}, dl[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = 4 * q + i;
                         if (wild) {
-                            const float top = stats[BQ + at + i];
-                            s[r] = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(a.c2, s[r] - top, -stats[3 * BQ + at + i]));
+                            const float top = stat[BQ + at + i];
+                            s[r] = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(a.c2, s[r] - top, -stat[3 * BQ + at + i]));
                         } else {
                             s[r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[r], -ls[i]));
                         }
@@ -294,11 +301,28 @@ __global__ __launch_bounds__(64 * WAVES) void k_grad_kv(const BackwardArgs b, in
                     const uint4 p = piece_of<T>(s, u), d = piece_of<T>(ds, u);
 #pragma unroll
                     for (int t = 0; t < DP / 32; ++t) {
-                        dv[t] = mma<T>(col_piece<T, DP>(gt, 32 * n, 32 * t, u, lane), p, dv[t]);
-                        dk[t] = mma<T>(col_piece<T, DP>(qt, 32 * n, 32 * t, u, lane), d, dk[t]);
+                        dv[t] = mma<T>(L::col_piece(gt, cl, n, t, u), p, dv[t]);
+                        dk[t] = mma<T>(L::col_piece(qt, cl, n, t, u), d, dk[t]);
                     }
                 }
             }
+        };
+        __syncthreads();  // the last head's tiles and bias are done with
+        stage_bias<T>(a, head, bias);
+        registers_loaded();
+        fetch(begin, 0);
+        for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
+            put(0);
+            loads_done();
+            __syncthreads();
+            fetch(i0 + BQ, 1);
+            step(lds, lds + kTile, stats, i0);
+            if (i0 + BQ >= nq) break;
+            put(1);
+            loads_done();
+            __syncthreads();
+            fetch(i0 + 2 * BQ, 0);
+            step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
         }
     }
     store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
@@ -334,11 +358,11 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     Carver c(ws);
     float *delta = c.take<float>(a.Nq * a.H);
     float *part = b.grad_table ? c.take<float>(nq * a.H * a.buckets) : nullptr;
-    const size_t tiles = 2 * BK * tile_stride<T, DP>() * sizeof(T), bias = (2 * a.reach + 1) * sizeof(float);
+    const size_t tiles = 4 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
     k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES, tiles + bias * (part ? 1 + WAVES : 1), s>>>(
         b, nq, delta, part);
     PYG_LAUNCH_CHECK();
-    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv), 64 * WAVES, tiles + 4 * BK * sizeof(float) + bias,
+    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv), 64 * WAVES, tiles + 8 * BK * sizeof(float) + bias,
                                   s>>>(b, nk, delta);
     PYG_LAUNCH_CHECK();
     if (part) {
@@ -352,7 +376,7 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
 template <typename T, int DP>
 int by_waves(const BackwardArgs &b, void *ws, hipStream_t s) {
     if (b.f.Nq <= 64 * b.f.B) return launch<T, DP, 1, 32>(b, ws, s);
-    return launch<T, DP, 4, 64>(b, ws, s);
+    return launch<T, DP, 4, DP * sizeof(T) <= 128 ? 64 : 32>(b, ws, s);
 }
 
 template <typename T>

@@ -46,7 +46,7 @@ struct FewTile {
             const int64_t key = j + 16 * u + m;
 #pragma unroll
             for (int s = 0; s < F::STEPS; ++s)
-                k[u][s] = load_piece<T>(kb + key * a.k_row, 4 * F::E * s + F::E * g, a.D, a.vec_k, key < end);
+                k[u][s] = load_piece<T>(kb + key * a.k_row, 4 * F::E * s + F::E * g, a.D, key < end);
 #pragma unroll
             for (int r = 0; r < 4; ++r) row(a, vb, j + 16 * u + 4 * g + r, end, m, v[4 * u + r]);
         }
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(const Args a, int64_t ns
     const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
     uint4 qf[F::STEPS];
 #pragma unroll
-    for (int s = 0; s < F::STEPS; ++s) qf[s] = load_piece<T>(qr, 4 * F::E * s + F::E * g, a.D, a.vec_q, there);
+    for (int s = 0; s < F::STEPS; ++s) qf[s] = load_piece<T>(qr, 4 * F::E * s + F::E * g, a.D, there);
 
     // the range of this workgroup's keys
     const int64_t len = (nk + splits - 1) / splits, begin = len * sp;
