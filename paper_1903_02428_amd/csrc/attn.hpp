@@ -36,8 +36,13 @@ __device__ __forceinline__ float to_f32(__bf16 v) { return static_cast<float>(v)
 // The bias over c of every offset, for head h, in LDS. Finite values stay
 // finite: a table entry of the type's lowest value masks without leaving the
 // row empty, as it does in the formula.
+// Returns, in every thread and after a barrier, whether any of it is so large that
+// c2 s - c2 m in one fused multiply-add leaves more than the exponent's own
+// rounding (tables of lowest values): s - m has to come first then.
+constexpr float kWild = 65536.f;
 template <typename T>
-__device__ __forceinline__ void stage_bias(const Args &a, int h, float *bias) {
+__device__ __forceinline__ bool stage_bias(const Args &a, int h, float *bias) {
+    int wild = 0;
     const T *t = static_cast<const T *>(a.table);
     for (int o = threadIdx.x; o <= 2 * a.reach; o += blockDim.x) {
         float v = 0.f;
@@ -49,7 +54,22 @@ __device__ __forceinline__ void stage_bias(const Args &a, int h, float *bias) {
             if (fabsf(raw) <= -kLowest) v = fminf(fmaxf(v, kLowest), -kLowest);
         }
         bias[o] = v;
+        wild |= fabsf(v) > kWild && fabsf(v) <= -kLowest;
     }
+    return __syncthreads_or(wild) != 0;
+}
+
+// A part of a kernel that comes in two forms: the inner one, for tiles that no mask, end or
+// varying bias touches, has no branches, so that its products and exponentials overlap.
+struct Inner {
+    static constexpr bool value = true;
+};
+struct Edge {
+    static constexpr bool value = false;
+};
+// Whether the offsets first .. last all lie in an end bucket, and none is masked.
+__device__ __forceinline__ bool flat(int first, int last, int reach, bool causal) {
+    return last <= -reach || (first >= reach && !causal);
 }
 
 // The other half's value of the same column (lanes l and l ^ 32).
@@ -75,6 +95,7 @@ __device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int d0
         for (int r = 0; r < 16; ++r) c[r] = v;
         return c;
     }
+    lane = opaque(lane);  // near the diagonal only: nothing of this is kept in registers for it
     const int m = lane & 31, h = lane >> 5, base = d0 + reach + (KEYS_IN_ROWS ? 4 * h - m : m - 4 * h);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -91,6 +112,7 @@ __device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int d0
 template <bool KEYS_IN_ROWS>
 __device__ __forceinline__ void mask_tile(f32x16 &c, int keys, int queries, bool causal, int d0, int lane) {
     if (keys >= 32 && queries >= 32 && (!causal || d0 + 31 <= 0)) return;
+    lane = opaque(lane);
     const int m = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -99,10 +121,6 @@ __device__ __forceinline__ void mask_tile(f32x16 &c, int keys, int queries, bool
         if (key >= keys || query >= queries || (causal && d0 + key - query > 0)) c[r] = kNegInf;
     }
 }
-
-// From this size on, c2 s - c2 m in one fused multiply-add leaves more than the
-// exponent's own rounding (a table of lowest values): s - m comes first there.
-constexpr float kWild = 65536.f;
 
 // Rows [first, last) of a [N, H, D] output, head h, get zeros (rows of no graph).
 template <typename T>

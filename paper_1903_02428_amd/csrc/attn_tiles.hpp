@@ -99,6 +99,13 @@ __device__ __forceinline__ int swizzle(int row) {
     else return (row & 3) << 2 | ((row >> 2) & 3);
 }
 
+// Hides a value from the compiler: what is derived from it is made again where it is
+// used (an instruction a read) and not kept in a register across the loop.
+__device__ __forceinline__ int opaque(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 template <typename T, int DP>
 struct Tile {
     static constexpr int E = Elem<T>::E, C = DP / E;
@@ -217,17 +224,10 @@ struct Stage {
     using L = Tile<T, DP>;
     static constexpr int E = L::E, C = L::C, kEach = ROWS * C / NT;
     static_assert(ROWS * C % NT == 0, "whole pieces for every thread");
-    uint32_t off[kEach];
     uint32_t row_bytes;
     int D;
     bool vec;
-    __device__ __forceinline__ Stage(int64_t stride, int D_, bool vec_) : row_bytes(stride * sizeof(T)), D(D_), vec(vec_) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int p = i * NT + threadIdx.x, row = p / C, d = ((p % C) ^ swizzle<C>(row)) * E;
-            off[i] = d < D ? row * row_bytes + d * sizeof(T) : kOutside;
-        }
-    }
+    __device__ __forceinline__ Stage(int64_t stride, int D_, bool vec_) : row_bytes(stride * sizeof(T)), D(D_), vec(vec_) {}
     // rows first .. of `head` (a [rows] array of this head's features); there are `left` of them
     __device__ __forceinline__ void load(const T *head, int64_t first, int64_t left, char *tile) const {
         const T *base = head + first * (row_bytes / sizeof(T));
@@ -238,7 +238,10 @@ struct Stage {
                              to_scalar(rows * row_bytes), 0x00020000u};
             const uint32_t wave = to_scalar(lds_offset(tile) + (threadIdx.x >> 6) * 1024u);
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) load_to_lds(rsrc, off[i], wave + i * NT * 16u);
+            for (int i = 0; i < kEach; ++i) {
+                const int p = i * NT + threadIdx.x, row = p / C, d = ((p % C) ^ swizzle<C>(row)) * E;
+                load_to_lds(rsrc, d < D ? row * row_bytes + d * sizeof(T) : kOutside, wave + i * NT * 16u);
+            }
         } else {
 #pragma unroll 1
             for (int p = threadIdx.x; p < ROWS * C; p += NT) {

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
     constexpr int kTile = L::template bytes<BK>();
     extern __shared__ __align__(16) char lds[];  // K and V of two tiles, the bias
     float *bias = reinterpret_cast<float *>(lds + 4 * kTile);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     // key heads vary fastest: with up to 8 of them (or a multiple) every XCD's L2 sees its own heads' keys only
     const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         if (a.zero_rest) zero_rows(out, q0, q0 + BM < pq.last ? q0 + BM : pq.last, a.H, head, a.D);
         return;
     }
-    stage_bias<T>(a, head, bias);
+    const bool wild = stage_bias<T>(a, head, bias);
     const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
                   k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
     const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
@@ -69,13 +69,24 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
     auto step = [&](const char *kt, const char *vt, int64_t j0) {
         const int d0 = near(j0 - shift), left = near(nk - j0);
         if (a.causal && d0 > 31) return;  // later than all of the wavefront's queries
+        // inner tiles: no mask, no end, one bias; they jump over what the others need
+        const bool inner = left >= BK && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
         f32x16 st[NK];
+        if (inner) {
+            const float flat_bias = bias[d0 > 0 ? 2 * a.reach : 0];
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            st[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
+            for (int n = 0; n < NK; ++n) st[n] = f32x16(flat_bias);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NK; ++n) st[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int s = 0; s < SQ; ++s) st[n] = mma<T>(L::row_piece(kt, rl, n, s), qf[s], st[n]);
-            mask_tile<true>(st[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+        if (!inner) {
+#pragma unroll
+            for (int n = 0; n < NK; ++n) mask_tile<true>(st[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
         }
         float t = kNegInf;
 #pragma unroll
@@ -91,22 +102,23 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
 #pragma unroll
             for (int u = 0; u < DP / 32; ++u) acc[u] *= shrink;
         }
-        if (__any(fabsf(ref) > kWild)) {
+        float z = -a.c2 * ref;
+        if (wild) {  // s - m first, and nothing left to subtract
 #pragma unroll
             for (int n = 0; n < NK; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) st[n][r] = __builtin_amdgcn_exp2f(a.c2 * (st[n][r] - ref));
-        } else {
-            const float z = -a.c2 * ref;
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) st[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, st[n][r], z));
+                for (int r = 0; r < 16; ++r) st[n][r] -= ref;
+            z = 0.f;
         }
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += st[n][r];
+            for (int r = 0; r < 16; ++r) {
+                st[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, st[n][r], z));
+                sum += st[n][r];
+            }
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int u = 0; u < Elem<T>::kSteps; ++u) {
                 // P is rounded to the operands' type for the matrix cores: at most half a step of that type on each
@@ -115,7 +127,6 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) acc[d] = mma<T>(L::col_piece(vt, cl, n, d, u), p, acc[d]);
             }
-        }
     };
     // the next tile is on its way to one half of the LDS while the other is worked on
     auto fetch = [&](int64_t j0, int half) {

@@ -21,9 +21,44 @@ __device__ __forceinline__ RowStat row_stat(float2 s, float c2) {
     return {s.x, s.y, s.x == kNegInf ? -kNegInf : fmaf(c2, s.x, s.y)};
 }
 
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// Adds a 32 x 32 tile of dS^T (rows keys, the lane's column a query) to the wavefront's sums
+// by offset (key - query). The tile is laid down in LDS and read along its 63 diagonals, a lane
+// each, so that no two lanes add to one place: LDS float atomics, a lane at a time, made the
+// tiles near the diagonal a fifth of the kernel (three graphs, 9,001 nodes, 16 heads of 64).
+constexpr int kSkewRow = 40, kSkew = 32 * kSkewRow;  // 40: the two halves' rows are 32 banks apart
+__device__ __forceinline__ void add_diagonals(const f32x16 &ds, float *own, float *skew, int d0, int reach, int lane) {
+    lane = opaque(lane);
+    const int m = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) skew[(8 * (r >> 2) + 4 * h + (r & 3)) * kSkewRow + m] = ds[r];
+    const int o = lane - 31;  // the lane's diagonal: key - query of the tile; lane 63 has none
+    float t = 0.f;
+#pragma unroll 8
+    for (int row = 0; row < 32; ++row) {
+        const int c = row - o;
+        const float v = skew[row * kSkewRow + (c & 31)];
+        t += static_cast<unsigned>(c) < 32u ? v : 0.f;
+    }
+    const int at = d0 + o;
+    const bool mine = lane < 63, low = mine && at < -reach, high = mine && at > reach;
+    if (mine && !low && !high) own[at + reach] += t;
+    // the ends stand for all offsets beyond them
+    const float below = wave_sum(low ? t : 0.f), above = wave_sum(high ? t : 0.f);
+    if (lane == 0) own[0] += below, own[2 * reach] += above;
+}
+
 // Wavefronts a SIMD that the registers have to leave room for.
 template <typename T, int DP>
-constexpr int kGradWaves = DP <= 64 ? 2 : 1;
+constexpr int kGradWaves = DP <= 64 || sizeof(T) == 2 ? 2 : 1;
+// The owned rows of V in LDS instead of registers: bf16 heads of 128 would need more than the 256 of two wavefronts a SIMD.
+template <typename T, int DP>
+constexpr bool kValuesInLds = DP == 128 && sizeof(T) == 2;
 
 // A workgroup owns 32 * WAVES queries, as in the forward.
 template <typename T, int DP, int WAVES, int BK>
@@ -36,7 +71,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     extern __shared__ __align__(16) char lds[];  // K and V of two tiles, the bias, the sums by offset
     float *bias = reinterpret_cast<float *>(lds + 4 * kTile);
     float *hist = bias + (2 * a.reach + 1);  // a wavefront's own sums by offset
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
     const int64_t slot = nslots - 1 - id / a.H;
@@ -51,10 +86,10 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         return;
     }
     const int offsets = 2 * a.reach + 1;
-    stage_bias<T>(a, head, bias);
     if (mine)
         for (int i = threadIdx.x; i < offsets * WAVES; i += NT) hist[i] = 0.f;
-    float *own = hist + wave * offsets;
+    const bool wild = stage_bias<T>(a, head, bias);
+    float *own = hist + wave * offsets, *skew = hist + WAVES * offsets + wave * kSkew;
     const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
                   k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
     const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
@@ -84,7 +119,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         if (h == 0) delta[row * a.H + head] = dl;
     }
     const RowStat st = row_stat(raw, a.c2);
-    const bool wild = __any(st.top != kNegInf && fabsf(st.top) > kWild);
+    const float minus = wild ? -st.log_sum : -st.lse;
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -101,51 +136,64 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     const typename L::ColLane cl(lane);
     const int64_t shift = i0 + nk - nq;
     auto step = [&](const char *kt, const char *vt, int64_t j0) {
+        const int d0 = near(j0 - shift), left = near(nk - j0);
+        if (a.causal && d0 > 31) return;
+        // inner tiles: no mask, no end, one bias; they jump over what the others need
+        const bool inner = left >= BK && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
+        f32x16 s[NK], dp[NK];
+        if (inner) {
+            const float flat_bias = bias[d0 > 0 ? 2 * a.reach : 0];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) s[n] = f32x16(flat_bias);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NK; ++n) s[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
+        }
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-            const int d0 = near(j0 + 32 * n - shift), left = near(nk - j0 - 32 * n);
-            if ((a.causal && d0 > 31) || left <= 0) continue;
-            f32x16 s = bias_tile<true>(bias, a.reach, d0, lane), dp = f32x16(0.f);
+            dp[n] = f32x16(0.f);
 #pragma unroll
             for (int u = 0; u < SQ; ++u) {
-                s = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s);
-                dp = mma<T>(L::row_piece(vt, rl, n, u), gf[u], dp);
+                s[n] = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s[n]);
+                dp[n] = mma<T>(L::row_piece(vt, rl, n, u), gf[u], dp[n]);
             }
-            mask_tile<true>(s, left, 32, a.causal, d0, lane);
-            if (wild) {
+        }
+        if (!inner) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = st.top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(a.c2, s[r] - st.top, -st.log_sum));
+            for (int n = 0; n < NK; ++n) mask_tile<true>(s[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+        }
+        if (wild) {  // s - top first, and only log2 sum left to subtract
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[n][r] = st.top == kNegInf ? kNegInf : s[n][r] - st.top;
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[n][r], minus)) * (dp[n][r] - dl);  // dS^T
+        if (mine) {
+            if (inner) {
+                float t = 0.f;
+#pragma unroll
+                for (int n = 0; n < NK; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) t += s[n][r];
+                (d0 > 0 ? above : below) += t;
             } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[r], -st.lse));
+                for (int n = 0; n < NK; ++n) add_diagonals(s[n], own, skew, d0 + 32 * n, a.reach, lane);
             }
+        }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] *= dp[r] - dl;  // dS^T
-            if (mine) {
-                if (d0 - 31 >= a.reach || d0 + 31 <= -a.reach) {
-                    float t = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) t += s[r];
-                    (d0 > 0 ? above : below) += t;
-                } else {
-                    // at most two lanes of an instruction meet in an offset: their column and row differ alike
-                    const int base = d0 + a.reach - m + 4 * h;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        int o = base + 8 * (r >> 2) + (r & 3);
-                        o = o < 0 ? 0 : o >= offsets ? offsets - 1 : o;
-                        atomicAdd(own + o, s[r]);
-                    }
-                }
-            }
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int u = 0; u < Elem<T>::kSteps; ++u) {
-                const uint4 p = piece_of<T>(s, u);  // dS rounded once to the operands' type
+                const uint4 p = piece_of<T>(s[n], u);  // dS rounded once to the operands' type
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) acc[t] = mma<T>(L::col_piece(kt, cl, n, t, u), p, acc[t]);
             }
-        }
     };
     auto fetch = [&](int64_t j0, int half) {
         if (j0 >= end) return;
@@ -167,7 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     }
     store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
     if (mine) {
-        for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o), above += __shfl_xor(above, o);
+        below = wave_sum(below), above = wave_sum(above);
         if (lane == 0) own[0] += below, own[offsets - 1] += above;
         __syncthreads();
         for (int i = threadIdx.x; i < a.buckets; i += NT) {
@@ -196,9 +244,11 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     constexpr int kTile = L::template bytes<BQ>();
     static_assert(BQ <= NT, "a thread a query's statistics");
     extern __shared__ __align__(16) char lds[];  // Q and dO of two tiles, their statistics, the bias
-    float *stats = reinterpret_cast<float *>(lds + 4 * kTile);  // [2][4][BQ]: lse, top, delta, log2 sum
-    float *bias = stats + 8 * BQ;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    constexpr bool VL = kValuesInLds<T, DP>;
+    char *vown = lds + 4 * kTile;
+    float *stats = reinterpret_cast<float *>(vown + (VL ? L::template bytes<BN>() : 0));  // [2][5][BQ]: lse, log2 sum, delta, delta, top
+    float *bias = stats + 10 * BQ;
+    const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv;
     const int64_t slot = id / a.Hkv;  // causal: the first keys are seen by the most queries
@@ -216,14 +266,17 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     const int64_t nq = q_last > q_first ? q_last - q_first : 0, nk = pk.last - pk.first;
     const int64_t j0 = pk.tile * BN + wave * 32, row = pk.first + j0 + m;
     const bool there = row < pk.last;
-    uint4 kf[SQ], vf[SQ];
+    uint4 kf[SQ], vf[VL ? 1 : SQ];
     const T *kr = static_cast<const T *>(a.k) + row * a.k_row + hk * a.k_head;
     const T *vr = static_cast<const T *>(a.v) + row * a.v_row + hk * a.v_head;
 #pragma unroll
     for (int s = 0; s < SQ; ++s) {
         kf[s] = load_piece<T>(kr, 2 * E * s + E * h, a.D, there);
-        vf[s] = load_piece<T>(vr, 2 * E * s + E * h, a.D, there);
+        if constexpr (!VL) vf[s] = load_piece<T>(vr, 2 * E * s + E * h, a.D, there);
     }
+    if constexpr (VL)
+        Stage<T, DP, BN, NT>(a.v_row, a.D, a.vec_v)
+            .load(static_cast<const T *>(a.v) + hk * a.v_head + pk.first * a.v_row, pk.tile * BN, nk - pk.tile * BN, vown);
     const int keys = near(nk - j0);
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -235,12 +288,14 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
         begin = begin < 0 ? 0 : begin / 32 * 32;
     }
     const Stage<T, DP, BQ, NT> sq(a.q_row, a.D, a.vec_q), sg((int64_t)a.H * a.D, a.D, a.vec_o);
-    const typename L::RowLane rl(lane);
-    const typename L::ColLane cl(lane);
+    const typename L::RowLane rows(lane);
+    const typename L::ColLane columns(lane);
+    const char *vmine = vown + wave * 32 * L::kRowBytes;
     for (int g = 0; g < a.G && begin < nq; ++g) {
         const int head = hk * a.G + g;
         const T *qb = static_cast<const T *>(a.q) + head * a.q_head + q_first * a.q_row;
         const T *gb = static_cast<const T *>(b.grad_out) + (q_first * a.H + head) * a.D;
+        bool wild = false;
         float2 next = make_float2(kNegInf, 0.f);
         float next_delta = 0.f;
         // Q and dO of the next tile go to the other half of the LDS, its statistics by way of registers
@@ -258,57 +313,81 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
         auto put = [&](int half) {
             if (threadIdx.x < BQ) {
                 const RowStat t = row_stat(next, a.c2);
-                float *s = stats + half * 4 * BQ + threadIdx.x;
-                s[0] = t.lse, s[BQ] = t.top, s[2 * BQ] = next_delta, s[3 * BQ] = t.log_sum;
+                float *s = stats + half * 5 * BQ + threadIdx.x;
+                s[0] = t.lse, s[BQ] = t.log_sum, s[2 * BQ] = s[3 * BQ] = next_delta, s[4 * BQ] = t.top;
             }
         };
+        // one form for all tiles, its accumulators being most of the registers: inner tiles jump over what they do not need
         auto step = [&](const char *qt, const char *gt, const float *stat, int64_t i0) {
+            const int d0 = near(j0 - (i0 + nk - nq)), left = near(nq - i0);
+            if (a.causal && d0 - (BQ - 1) > 31) return;  // all of the wavefront's keys come later than all queries
+            const bool inner = left >= BQ && keys >= 32 && flat(d0 - (BQ - 1), d0 + 31, a.reach, a.causal);
+            f32x16 s[NQ], dp[NQ];
+            typename L::RowLane rl = rows;
+            typename L::ColLane cl = columns;
+            rl.x = opaque(rl.x), cl.x = opaque(cl.x);
+            if (inner) {
+                const float flat_bias = bias[d0 > 0 ? 2 * a.reach : 0];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[n] = f32x16(flat_bias);
+            } else {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[n] = bias_tile<false>(bias, a.reach, d0 - 32 * n, lane);
+            }
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                const int d0 = near(j0 - (i0 + 32 * n + nk - nq)), left = near(nq - i0 - 32 * n);
-                if ((a.causal && d0 > 31) || left <= 0) continue;
-                f32x16 s = bias_tile<false>(bias, a.reach, d0, lane), dp = f32x16(0.f);
+                dp[n] = f32x16(0.f);
 #pragma unroll
                 for (int u = 0; u < SQ; ++u) {
-                    s = mma<T>(L::row_piece(qt, rl, n, u), kf[u], s);
-                    dp = mma<T>(L::row_piece(gt, rl, n, u), vf[u], dp);
+                    s[n] = mma<T>(L::row_piece(qt, rl, n, u), kf[u], s[n]);
+                    dp[n] = mma<T>(L::row_piece(gt, rl, n, u), VL ? L::row_piece(vmine, rl, 0, u) : vf[VL ? 0 : u], dp[n]);
                 }
-                mask_tile<false>(s, keys, left, a.causal, d0, lane);
-                const float *tops = stat + BQ + 32 * n;
-                const float my_top = tops[m];
-                const bool wild = __any(my_top != kNegInf && fabsf(my_top) > kWild);
-                f32x16 ds;
+            }
+            if (!inner) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) mask_tile<false>(s[n], keys, left - 32 * n, a.causal, d0 - 32 * n, lane);
+            }
+            const float *mine = stat + opaque(4 * h);
+            if (wild) {
+                // s - top first, and only log2 sum left to subtract
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float top = mine[4 * BQ + 32 * n + 8 * (r >> 2) + (r & 3)];
+                        s[n][r] = top == kNegInf ? kNegInf : s[n][r] - top;
+                    }
+                mine += BQ;  // log2 sum where the others have lse, and delta once more
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int at = 32 * n + 8 * q + 4 * h;
-                    const float4 l = *reinterpret_cast<const float4 *>(stat + at);
-                    const float4 e = *reinterpret_cast<const float4 *>(stat + 2 * BQ + at);
+                    const float *at = mine + 32 * n + 8 * q;
+                    const float4 l = *reinterpret_cast<const float4 *>(at);
+                    const float4 e = *reinterpret_cast<const float4 *>(at + 2 * BQ);
                     const float ls[4] = {l.x, l.y, l.z, l.w}, dl[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = 4 * q + i;
-                        if (wild) {
-                            const float top = stat[BQ + at + i];
-                            s[r] = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(fmaf(a.c2, s[r] - top, -stat[3 * BQ + at + i]));
-                        } else {
-                            s[r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[r], -ls[i]));
-                        }
-                        ds[r] = s[r] * (dp[r] - dl[i]);
+                        s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[n][r], -ls[i]));
+                        dp[n][r] = s[n][r] * (dp[n][r] - dl[i]);  // dS
                     }
                 }
 #pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
                 for (int u = 0; u < Elem<T>::kSteps; ++u) {
-                    const uint4 p = piece_of<T>(s, u), d = piece_of<T>(ds, u);
+                    const uint4 p = piece_of<T>(s[n], u), d = piece_of<T>(dp[n], u);
 #pragma unroll
                     for (int t = 0; t < DP / 32; ++t) {
                         dv[t] = mma<T>(L::col_piece(gt, cl, n, t, u), p, dv[t]);
                         dk[t] = mma<T>(L::col_piece(qt, cl, n, t, u), d, dk[t]);
                     }
                 }
-            }
         };
         __syncthreads();  // the last head's tiles and bias are done with
-        stage_bias<T>(a, head, bias);
+        wild = stage_bias<T>(a, head, bias);
         registers_loaded();
         fetch(begin, 0);
         for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
@@ -322,7 +401,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             loads_done();
             __syncthreads();
             fetch(i0 + 2 * BQ, 0);
-            step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
+            step(lds + 2 * kTile, lds + 3 * kTile, stats + 5 * BQ, i0 + BQ);
         }
     }
     store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
@@ -359,10 +438,10 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     float *delta = c.take<float>(a.Nq * a.H);
     float *part = b.grad_table ? c.take<float>(nq * a.H * a.buckets) : nullptr;
     const size_t tiles = 4 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
-    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES, tiles + bias * (part ? 1 + WAVES : 1), s>>>(
+    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES, tiles + bias * (part ? 1 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(
         b, nq, delta, part);
     PYG_LAUNCH_CHECK();
-    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv), 64 * WAVES, tiles + 8 * BK * sizeof(float) + bias,
+    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv), 64 * WAVES, tiles + (kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0) + 10 * BK * sizeof(float) + bias,
                                   s>>>(b, nk, delta);
     PYG_LAUNCH_CHECK();
     if (part) {

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(const Args a, int64_t ns
     constexpr int W = F::W;
     __shared__ float lo[kFewWaves][16][DP + 1];
     __shared__ float lt[kFewWaves][16], ls[kFewWaves][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
     const int64_t id = blockIdx.x;
     const int hk = id % a.Hkv;
     const int sp = static_cast<int>(id / a.Hkv % splits);
