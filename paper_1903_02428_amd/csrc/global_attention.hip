@@ -70,13 +70,12 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         const int d0 = near(j0 - shift), left = near(nk - j0);
         if (a.causal && d0 > 31) return;  // later than all of the wavefront's queries
         // inner tiles: no mask, no end, one bias; they jump over what the others need
-        const bool inner = left >= BK && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
+        const bool inner = left >= BK && !wild && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
+        const float constant = inner ? bias[d0 > 0 ? 2 * a.reach : 0] : 0.f;  // the bias of an inner tile
         f32x16 st[NK];
-        if (inner) {
-            const float flat_bias = bias[d0 > 0 ? 2 * a.reach : 0];
 #pragma unroll
-            for (int n = 0; n < NK; ++n) st[n] = f32x16(flat_bias);
-        } else {
+        for (int n = 0; n < NK; ++n) st[n] = f32x16(0.f);
+        if (!inner) {
 #pragma unroll
             for (int n = 0; n < NK; ++n) st[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
         }
@@ -93,7 +92,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) t = fmaxf(t, st[n][r]);
-        t = fmaxf(t, other_half(t));
+        t = fmaxf(t, other_half(t)) + constant;
         const float top_new = fmaxf(top, t), ref = top_new == kNegInf ? 0.f : top_new;
         const float shrink = __builtin_amdgcn_exp2f(a.c2 * (top - ref));
         top = top_new;
@@ -102,7 +101,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
 #pragma unroll
             for (int u = 0; u < DP / 32; ++u) acc[u] *= shrink;
         }
-        float z = -a.c2 * ref;
+        float z = a.c2 * (constant - ref);
         if (wild) {  // s - m first, and nothing left to subtract
 #pragma unroll
             for (int n = 0; n < NK; ++n)

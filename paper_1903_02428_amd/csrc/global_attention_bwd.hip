@@ -13,12 +13,15 @@ namespace pyg {
 namespace attn {
 namespace {
 
-// exp2 of a score tile's registers, normalised: exp2(c2 (s - top) - log2 sum).
+// A row's statistics in units of s: p = exp2(c2 (s + start)), start = -(top + log2 sum / c2), which a tile's
+// accumulators begin with, as -delta does dP's; -infinity for a row that sees no key. Where the bias holds
+// lowest values (wild) s - top comes first: start = -log2 sum / c2 is added after it.
 struct RowStat {
-    float top, log_sum, lse;  // lse = c2 top + log2 sum, infinite for a row that sees no key
+    float top, start, rest;
 };
 __device__ __forceinline__ RowStat row_stat(float2 s, float c2) {
-    return {s.x, s.y, s.x == kNegInf ? -kNegInf : fmaf(c2, s.x, s.y)};
+    const float rest = -s.y / c2;
+    return {s.x, s.x == kNegInf ? kNegInf : rest - s.x, rest};
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         if (h == 0) delta[row * a.H + head] = dl;
     }
     const RowStat st = row_stat(raw, a.c2);
-    const float minus = wild ? -st.log_sum : -st.lse;
+    const f32x16 no_delta(-dl);  // dP starts from it, but where registers are short
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -139,40 +142,40 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         const int d0 = near(j0 - shift), left = near(nk - j0);
         if (a.causal && d0 > 31) return;
         // inner tiles: no mask, no end, one bias; they jump over what the others need
-        const bool inner = left >= BK && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
+        const bool inner = left >= BK && !wild && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
         f32x16 s[NK], dp[NK];
         if (inner) {
-            const float flat_bias = bias[d0 > 0 ? 2 * a.reach : 0];
+            const float begin = bias[d0 > 0 ? 2 * a.reach : 0] + st.start;
 #pragma unroll
-            for (int n = 0; n < NK; ++n) s[n] = f32x16(flat_bias);
+            for (int n = 0; n < NK; ++n) s[n] = f32x16(begin);
         } else {
 #pragma unroll
-            for (int n = 0; n < NK; ++n) s[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
-        }
-#pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            dp[n] = f32x16(0.f);
-#pragma unroll
-            for (int u = 0; u < SQ; ++u) {
-                s[n] = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s[n]);
-                dp[n] = mma<T>(L::row_piece(vt, rl, n, u), gf[u], dp[n]);
+            for (int n = 0; n < NK; ++n) {
+                s[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
+                if (!wild) s[n] += st.start;
             }
-        }
-        if (!inner) {
-#pragma unroll
-            for (int n = 0; n < NK; ++n) mask_tile<true>(s[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
-        }
-        if (wild) {  // s - top first, and only log2 sum left to subtract
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[n][r] = st.top == kNegInf ? kNegInf : s[n][r] - st.top;
         }
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[n][r], minus)) * (dp[n][r] - dl);  // dS^T
+            for (int u = 0; u < SQ; ++u) {
+                s[n] = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s[n]);
+                dp[n] = mma<T>(L::row_piece(vt, rl, n, u), gf[u], u == 0 ? (DP < 128 ? no_delta : f32x16(0.f)) : dp[n]);
+            }
+        if (!inner) {
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                if (wild) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[n][r] = st.top == kNegInf ? kNegInf : (s[n][r] - st.top) + st.rest;
+                }
+                mask_tile<true>(s[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[n][r] = __builtin_amdgcn_exp2f(a.c2 * s[n][r]) * (DP < 128 ? dp[n][r] : dp[n][r] - dl);  // dS^T
         if (mine) {
             if (inner) {
                 float t = 0.f;
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
 // dK^T = Q^T dS as they stand.
 template <typename T, int DP, int WAVES, int BQ>
 __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(const BackwardArgs b, int64_t nslots,
-                                                        const float *__restrict__ delta) {
+                                                        const float *__restrict__ delta, int splits, float *__restrict__ part) {
     const Args &a = b.f;
     constexpr int NT = 64 * WAVES, BN = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NQ = BQ / 32;
     using L = Tile<T, DP>;
@@ -246,19 +249,26 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     extern __shared__ __align__(16) char lds[];  // Q and dO of two tiles, their statistics, the bias
     constexpr bool VL = kValuesInLds<T, DP>;
     char *vown = lds + 4 * kTile;
-    float *stats = reinterpret_cast<float *>(vown + (VL ? L::template bytes<BN>() : 0));  // [2][5][BQ]: lse, log2 sum, delta, delta, top
-    float *bias = stats + 10 * BQ;
+    float *stats = reinterpret_cast<float *>(vown + (VL ? L::template bytes<BN>() : 0));  // [2][4][BQ]: start, -delta, top, rest
+    float *bias = stats + 8 * BQ;
     const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     const uint32_t id = blockIdx.x;
-    const int hk = id % a.Hkv;
-    const int64_t slot = id / a.Hkv;  // causal: the first keys are seen by the most queries
+    const int hk = id % a.Hkv, sp = id / a.Hkv % splits, heads = a.G / splits;  // the workgroup's share of the G heads
+    const int64_t slot = id / a.Hkv / splits;  // causal: the first keys are seen by the most queries
+    const int64_t whole = a.Nk * a.Hkv * a.D;
+    float *dk_part = part + 2 * sp * whole, *dv_part = dk_part + whole;  // where there are several
     const Place pk = place_of(a.k_ptr, a.B, a.Nk, slot, BN, 1, lane);
     const int64_t k0 = pk.first + pk.tile * BN;
     if (pk.tile < 0 || k0 >= pk.last) return;
     if (pk.graph == a.B) {
         const int64_t e = k0 + BN < pk.last ? k0 + BN : pk.last;
-        zero_rows(static_cast<T *>(b.grad_k), k0, e, a.Hkv, hk, a.D);
-        zero_rows(static_cast<T *>(b.grad_v), k0, e, a.Hkv, hk, a.D);
+        if (splits > 1) {
+            zero_rows(dk_part, k0, e, a.Hkv, hk, a.D);
+            zero_rows(dv_part, k0, e, a.Hkv, hk, a.D);
+        } else {
+            zero_rows(static_cast<T *>(b.grad_k), k0, e, a.Hkv, hk, a.D);
+            zero_rows(static_cast<T *>(b.grad_v), k0, e, a.Hkv, hk, a.D);
+        }
         return;
     }
     const int64_t q_first = uniform64(ptr_at(a.q_ptr, pk.graph, a.Nq)),
@@ -291,88 +301,83 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     const typename L::RowLane rows(lane);
     const typename L::ColLane columns(lane);
     const char *vmine = vown + wave * 32 * L::kRowBytes;
-    for (int g = 0; g < a.G && begin < nq; ++g) {
+    for (int g = sp * heads; g < (sp + 1) * heads && begin < nq; ++g) {
         const int head = hk * a.G + g;
         const T *qb = static_cast<const T *>(a.q) + head * a.q_head + q_first * a.q_row;
         const T *gb = static_cast<const T *>(b.grad_out) + (q_first * a.H + head) * a.D;
         bool wild = false;
-        float2 next = make_float2(kNegInf, 0.f);
+        float2 next{};
         float next_delta = 0.f;
+        const int query = threadIdx.x % BQ;
         // Q and dO of the next tile go to the other half of the LDS, its statistics by way of registers
         auto fetch = [&](int64_t i0, int half) {
             if (i0 >= nq) return;
+            // every thread loads (the last query's where there is none): a branch here would have the compiler wait for
+            // the old values' registers, and with them for the tiles
+            const int64_t last = nq - 1 - i0, r = i0 + (last < query ? last : query);
+            next = *reinterpret_cast<const float2 *>(a.stat + ((q_first + r) * a.H + head) * 2);
+            next_delta = delta[(q_first + r) * a.H + head];
             sq.load(qb, i0, nq - i0, lds + 2 * half * kTile);
             sg.load(gb, i0, nq - i0, lds + (2 * half + 1) * kTile);
-            const int64_t r = i0 + threadIdx.x;
-            next = make_float2(kNegInf, 0.f), next_delta = 0.f;
-            if (threadIdx.x < BQ && r < nq) {
-                next = *reinterpret_cast<const float2 *>(a.stat + ((q_first + r) * a.H + head) * 2);
-                next_delta = delta[(q_first + r) * a.H + head];
-            }
         };
-        auto put = [&](int half) {
-            if (threadIdx.x < BQ) {
-                const RowStat t = row_stat(next, a.c2);
-                float *s = stats + half * 5 * BQ + threadIdx.x;
-                s[0] = t.lse, s[BQ] = t.log_sum, s[2 * BQ] = s[3 * BQ] = next_delta, s[4 * BQ] = t.top;
-            }
+        auto put = [&](int64_t i0, int half) {
+            const RowStat t = row_stat(make_float2(i0 + query < nq ? next.x : kNegInf, next.y), a.c2);
+            float *s = stats + half * 4 * BQ + query;
+            s[0] = t.start, s[BQ] = -next_delta, s[2 * BQ] = t.top, s[3 * BQ] = t.rest;  // the same from several threads
         };
         // one form for all tiles, its accumulators being most of the registers: inner tiles jump over what they do not need
         auto step = [&](const char *qt, const char *gt, const float *stat, int64_t i0) {
             const int d0 = near(j0 - (i0 + nk - nq)), left = near(nq - i0);
             if (a.causal && d0 - (BQ - 1) > 31) return;  // all of the wavefront's keys come later than all queries
-            const bool inner = left >= BQ && keys >= 32 && flat(d0 - (BQ - 1), d0 + 31, a.reach, a.causal);
+            const bool inner = left >= BQ && keys >= 32 && !wild && flat(d0 - (BQ - 1), d0 + 31, a.reach, a.causal);
             f32x16 s[NQ], dp[NQ];
             typename L::RowLane rl = rows;
             typename L::ColLane cl = columns;
             rl.x = opaque(rl.x), cl.x = opaque(cl.x);
-            if (inner) {
-                const float flat_bias = bias[d0 > 0 ? 2 * a.reach : 0];
+            const float *mine = stat + opaque(4 * h);
+            const float constant = inner ? a.c2 * bias[d0 > 0 ? 2 * a.reach : 0] : 0.f;  // the bias of an inner tile
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) s[n] = f32x16(flat_bias);
-            } else {
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) s[n] = bias_tile<false>(bias, a.reach, d0 - 32 * n, lane);
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(mine + 32 * n + 8 * q);
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(mine + BQ + 32 * n + 8 * q);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][4 * q + i] = x[i], dp[n][4 * q + i] = y[i];
+                }
+            if (!inner) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    const f32x16 b = bias_tile<false>(bias, a.reach, d0 - 32 * n, lane);
+                    s[n] = wild ? b : s[n] + b;
+                }
             }
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                dp[n] = f32x16(0.f);
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int u = 0; u < SQ; ++u) {
                     s[n] = mma<T>(L::row_piece(qt, rl, n, u), kf[u], s[n]);
                     dp[n] = mma<T>(L::row_piece(gt, rl, n, u), VL ? L::row_piece(vmine, rl, 0, u) : vf[VL ? 0 : u], dp[n]);
                 }
-            }
             if (!inner) {
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) mask_tile<false>(s[n], keys, left - 32 * n, a.causal, d0 - 32 * n, lane);
-            }
-            const float *mine = stat + opaque(4 * h);
-            if (wild) {
-                // s - top first, and only log2 sum left to subtract
+                for (int n = 0; n < NQ; ++n) {
+                    if (wild) {
 #pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float top = mine[4 * BQ + 32 * n + 8 * (r >> 2) + (r & 3)];
-                        s[n][r] = top == kNegInf ? kNegInf : s[n][r] - top;
+                        for (int r = 0; r < 16; ++r) {
+                            const float *at = mine + 2 * BQ + 32 * n + 8 * (r >> 2) + (r & 3);
+                            s[n][r] = at[0] == kNegInf ? kNegInf : (s[n][r] - at[0]) + at[BQ];
+                        }
                     }
-                mine += BQ;  // log2 sum where the others have lse, and delta once more
+                    mask_tile<false>(s[n], keys, left - 32 * n, a.causal, d0 - 32 * n, lane);
+                }
             }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float *at = mine + 32 * n + 8 * q;
-                    const float4 l = *reinterpret_cast<const float4 *>(at);
-                    const float4 e = *reinterpret_cast<const float4 *>(at + 2 * BQ);
-                    const float ls[4] = {l.x, l.y, l.z, l.w}, dl[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 4 * q + i;
-                        s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[n][r], -ls[i]));
-                        dp[n][r] = s[n][r] * (dp[n][r] - dl[i]);  // dS
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[n][r], constant));
+                    dp[n][r] *= s[n][r];  // dS
                 }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
@@ -391,22 +396,51 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
         registers_loaded();
         fetch(begin, 0);
         for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
-            put(0);
+            put(i0, 0);
             loads_done();
             __syncthreads();
             fetch(i0 + BQ, 1);
             step(lds, lds + kTile, stats, i0);
             if (i0 + BQ >= nq) break;
-            put(1);
+            put(i0 + BQ, 1);
             loads_done();
             __syncthreads();
             fetch(i0 + 2 * BQ, 0);
-            step(lds + 2 * kTile, lds + 3 * kTile, stats + 5 * BQ, i0 + BQ);
+            step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
         }
     }
-    store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
-    store_rows<T, DP>(static_cast<T *>(b.grad_v), row, there, a.Hkv, hk, a.D, a.vec_o, dv, 1.f, lane);
+    if (splits > 1) {
+        store_rows<float, DP>(dk_part, row, there, a.Hkv, hk, a.D, a.D % 4 == 0, dk, a.scale, lane);
+        store_rows<float, DP>(dv_part, row, there, a.Hkv, hk, a.D, a.D % 4 == 0, dv, 1.f, lane);
+    } else {
+        store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
+        store_rows<T, DP>(static_cast<T *>(b.grad_v), row, there, a.Hkv, hk, a.D, a.vec_o, dv, 1.f, lane);
+    }
 }
+
+// dK and dV from the shares of the head groups [splits][2][Nk, Hkv, D], in order.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_join_kv(const float *__restrict__ part, int64_t n, int splits,
+                                                    T *__restrict__ dk, T *__restrict__ dv) {
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+        float x = 0.f, y = 0.f;
+        for (int s = 0; s < splits; ++s) x += part[2 * s * n + i], y += part[(2 * s + 1) * n + i];
+        dk[i] = T(x), dv[i] = T(y);
+    }
+}
+
+// Where few key tiles leave the card idle, the G heads that share a key head are
+// dealt out over several workgroups: up to 1,024 (two rounds of two a CU). 8,192 ordered nodes, 16 heads of
+// 128 on 4: one workgroup a tile 513 us, four and their sum 281 us.
+int kv_splits(const Args &a, int64_t tiles) {
+    int s = 1;
+    while (s < a.G && tiles * a.Hkv * s < 1024) {
+        do ++s;
+        while (a.G % s);
+    }
+    return s;
+}
+int64_t key_tiles(const Args &a) { return a.Nk / 128 + 1; }
 
 // dT[b, h] from the workgroups' shares [slots, H, buckets], in a fixed order: 64
 // slots in turn by each of the workgroup's rows of threads, then the rows.
@@ -434,16 +468,27 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     const Args &a = b.f;
     const int64_t nq = slots(a.Nq, a.B, 32 * WAVES), nk = slots(a.Nk, a.B, 32 * WAVES);
     if (nq * a.H * 64 * WAVES > kMost || nk * a.Hkv * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
+    const int splits = WAVES == 1 ? 1 : kv_splits(a, key_tiles(a));
+    if (nk * a.Hkv * splits * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
     Carver c(ws);
     float *delta = c.take<float>(a.Nq * a.H);
-    float *part = b.grad_table ? c.take<float>(nq * a.H * a.buckets) : nullptr;
+    float *part = c.take<float>(b.grad_table ? nq * a.H * a.buckets : 0);
+    float *kv_part = c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
+    if (!b.grad_table) part = nullptr;
     const size_t tiles = 4 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
-    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES, tiles + bias * (part ? 1 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(
-        b, nq, delta, part);
+    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES,
+                                 tiles + bias * (part ? 1 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(b, nq, delta, part);
     PYG_LAUNCH_CHECK();
-    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv), 64 * WAVES, tiles + (kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0) + 10 * BK * sizeof(float) + bias,
-                                  s>>>(b, nk, delta);
+    const size_t own = kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0;
+    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv * splits), 64 * WAVES,
+                                  tiles + own + 8 * BK * sizeof(float) + bias, s>>>(b, nk, delta, splits, kv_part);
     PYG_LAUNCH_CHECK();
+    if (splits > 1) {
+        const int64_t n = a.Nk * a.Hkv * a.D;
+        k_join_kv<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(kv_part, n, splits, static_cast<T *>(b.grad_k),
+                                                                  static_cast<T *>(b.grad_v));
+        PYG_LAUNCH_CHECK();
+    }
     if (part) {
         k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), kBlock, 0, s>>>(part, nq, a.H, a.buckets,
                                                                             static_cast<T *>(b.grad_table));
@@ -471,6 +516,8 @@ size_t backward_workspace(const Args &a) {
     Carver c(nullptr);
     c.take<float>(a.Nq * a.H);
     c.take<float>(slots(a.Nq, a.B, 32) * a.H * a.buckets);  // the smallest tiles have the most slots
+    const int splits = kv_splits(a, key_tiles(a));
+    c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
     return align_up(c.used, 256);
 }
 

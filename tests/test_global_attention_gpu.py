@@ -69,6 +69,9 @@ CASES = [
     ([700], [257], 2, 2, 32, 8, 16, True),
     ([130, 250], None, 3, 1, 7, 2, 1, False),
     ([190], [333], 1, 1, 1, 0, 0, False),
+    # heads of a group dealt out over workgroups (few key tiles): all of them, and a part
+    ([150, 140], None, 6, 1, 40, 8, 16, True),
+    ([260], [140], 8, 2, 64, 4, 8, False),
 ]
 
 
