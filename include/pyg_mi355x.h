@@ -752,7 +752,9 @@ int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
 /* out[i, h] = sum_j p_ij v[j, h'], p_i = softmax over the keys j of i's graph of
  * scale <q[i, h], k[j, h']> + T[bucket(j - (i + nk - nq)), h].
  *   q [Nq, H, D], k and v [Nk, Hkv, D] with the strides of *a; out [Nq, H, D] contiguous;
- *   stat  fp32 [Nq, H, 2] or NULL: what the backward needs of every row.
+ *   stat  fp32 [Nq, H, 2] or NULL: what the backward needs of every row;
+ *   rest  [Nq, H, D] or NULL, bf16 only: what rounding took from out (the backward's row sums are
+ *         as exact with it as if out had 16 bits more).
  * A row that sees no key (none in its graph, all masked, all entries -infinity)
  * gives zeros, and zero gradients. Scores, sums and statistics are fp32; bf16
  * weights p are rounded to bf16 for the second product. Deterministic.
@@ -761,18 +763,18 @@ int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
  * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 4096, rows >= 2^31, a grid
  * beyond 2^32 threads), PYG_ERR_WORKSPACE. */
 int pyg_global_attention(const pyg_attention *a, const void *q, const void *k, const void *v, void *out, float *stat,
-                         void *ws, size_t ws_bytes, void *stream);
+                         void *rest, void *ws, size_t ws_bytes, void *stream);
 
 /* Workspace bytes needed by pyg_global_attention_backward. */
 int pyg_global_attention_backward_workspace(const pyg_attention *a, size_t *bytes);
 
-/* Gradients of the above from grad_out [Nq, H, D], the inputs, `out` and `stat` of the
- * forward: grad_q [Nq, H, D], grad_k and grad_v [Nk, Hkv, D] (summed over the heads that
+/* Gradients of the above from grad_out [Nq, H, D], the inputs, `out`, `stat` and `rest` (or
+ * NULL) of the forward: grad_q [Nq, H, D], grad_k and grad_v [Nk, Hkv, D] (summed over the heads that
  * share a key head in fp32), grad_table [buckets, H] or NULL, all contiguous, in dtype.
  * Rows of no graph get zeros. Deterministic. Errors: as above. */
 int pyg_global_attention_backward(const pyg_attention *a, const void *grad_out, const void *q, const void *k,
-                                  const void *v, const void *out, const float *stat, void *grad_q, void *grad_k,
-                                  void *grad_v, void *grad_table, void *ws, size_t ws_bytes, void *stream);
+                                  const void *v, const void *out, const float *stat, const void *rest, void *grad_q,
+                                  void *grad_k, void *grad_v, void *grad_table, void *ws, size_t ws_bytes, void *stream);
 
 /* ---- The norms around a block, with its gate and residual scale. */
 

@@ -165,9 +165,9 @@ def library() -> ctypes.CDLL:
             "pyg_global_pool_workspace": [i32, i64, i64, i64, i32, sz],
             "pyg_global_pool": [p, i32, i64, i64, p, i64, i32, p, p, p, ctypes.c_size_t, p],
             "pyg_global_attention_workspace": [ctypes.POINTER(_Attention), sz],
-            "pyg_global_attention": [ctypes.POINTER(_Attention), p, p, p, p, p, p, ctypes.c_size_t, p],
+            "pyg_global_attention": [ctypes.POINTER(_Attention), p, p, p, p, p, p, p, ctypes.c_size_t, p],
             "pyg_global_attention_backward_workspace": [ctypes.POINTER(_Attention), sz],
-            "pyg_global_attention_backward": [ctypes.POINTER(_Attention), p, p, p, p, p, p, p, p, p, p, p,
+            "pyg_global_attention_backward": [ctypes.POINTER(_Attention), p, p, p, p, p, p, p, p, p, p, p, p,
                                               ctypes.c_size_t, p],
             "pyg_block_norm": [ctypes.POINTER(_BlockNorm), p, p, p, p, p],
             "pyg_block_norm_backward_workspace": [ctypes.POINTER(_BlockNorm), sz],

@@ -25,6 +25,7 @@ struct Args {
     int buckets, reach;
     const void *q, *k, *v;
     void *out;
+    void *rest;   // [Nq, H, D], bf16 only: what rounding took from out, itself rounded; or NULL
     float *stat;  // [Nq, H, 2]: the row's largest s, log2 of its sum of exp2(c2 (s - m)); or NULL
 };
 
@@ -133,11 +134,13 @@ __device__ __forceinline__ void zero_rows(T *out, int64_t first, int64_t last, i
 }
 
 // out[row, head h] from a wavefront's D x 32 result (lane: column = row, registers = features), times `mul`.
-template <typename T, int DP>
+// REST: what the results lose to the type's rounding instead.
+template <typename T, int DP, bool REST = false>
 __device__ __forceinline__ void store_rows(T *out, int64_t row, bool there, int H, int h, int D, bool vec,
                                            const f32x16 (&acc)[DP / 32], float mul, int lane) {
     if (!there) return;
     T *o = out + (row * H + h) * D;
+    const auto value = [&](float v) { return REST ? v * mul - to_f32(T(v * mul)) : v * mul; };
     const int hh = lane >> 5;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
@@ -145,8 +148,8 @@ __device__ __forceinline__ void store_rows(T *out, int64_t row, bool there, int 
         for (int r = 0; r < 4; ++r) {
             const int d = 32 * t + 8 * r + 4 * hh;
             if (d >= D) continue;
-            const float v0 = acc[t][4 * r] * mul, v1 = acc[t][4 * r + 1] * mul, v2 = acc[t][4 * r + 2] * mul,
-                        v3 = acc[t][4 * r + 3] * mul;
+            const float v0 = value(acc[t][4 * r]), v1 = value(acc[t][4 * r + 1]), v2 = value(acc[t][4 * r + 2]),
+                        v3 = value(acc[t][4 * r + 3]);
             if (vec) {
                 if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(o + d) = make_uint2(pack_bf16(v0, v1), pack_bf16(v2, v3));
                 else *reinterpret_cast<float4 *>(o + d) = make_float4(v0, v1, v2, v3);

@@ -189,6 +189,30 @@ __device__ __forceinline__ uint4 load_piece(const T *__restrict__ row, int d, in
                       static_cast<uint32_t>(hi >> 32));
 }
 
+// A lane's row as operand pieces (features 2 E s + E h .. in piece s); `row` can be
+// read in any case, `there` says whether it counts. Widths of whole pieces are read without a branch, so
+// that all loads are under way together.
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T *__restrict__ row, int D, bool there, int h, uint4 (&p)[N]) {
+    constexpr int E = Elem<T>::E;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef u32x4 __attribute__((aligned(2))) any;
+    if (D % E == 0) {
+        u32x4 v[N];
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            const int d = 2 * E * s + E * h;
+            v[s] = *reinterpret_cast<const any *>(row + (d < D ? d : 0));
+        }
+#pragma unroll
+        for (int s = 0; s < N; ++s)
+            p[s] = there && 2 * E * s + E * h < D ? make_uint4(v[s][0], v[s][1], v[s][2], v[s][3]) : make_uint4(0, 0, 0, 0);
+        return;
+    }
+#pragma unroll
+    for (int s = 0; s < N; ++s) p[s] = load_piece<T>(row, 2 * E * s + E * h, D, there);
+}
+
 // ROWS rows of one head, from memory to an LDS tile by a workgroup of NT
 // threads. 16-byte rows (vec) go without passing registers
 // (buffer_load_dwordx4 .. lds: 64 lanes write 1 KB in a row): the swizzle is in which

@@ -46,11 +46,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
     const int64_t row = pq.first + i0 + m;        // the lane's query row
     const bool there = row < pq.last;
     uint4 qf[SQ];
-    {
-        const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
-#pragma unroll
-        for (int s = 0; s < SQ; ++s) qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, there);
-    }
+    load_row(static_cast<const T *>(a.q) + (there ? row : pq.first) * a.q_row + head * a.q_head, a.D, there, h, qf);
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -147,7 +143,10 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
     }
     sum += other_half(sum);
-    store_rows<T, DP>(out, row, there, a.H, head, a.D, a.vec_o, acc, top == kNegInf ? 0.f : 1.f / sum, lane);
+    const float mul = top == kNegInf ? 0.f : 1.f / sum;
+    store_rows<T, DP>(out, row, there, a.H, head, a.D, a.vec_o, acc, mul, lane);
+    if constexpr (sizeof(T) == 2)
+        if (a.rest) store_rows<T, DP, true>(static_cast<T *>(a.rest), row, there, a.H, head, a.D, a.vec_o, acc, mul, lane);
     if (a.stat && there && h == 0)
         *reinterpret_cast<float2 *>(a.stat + (row * a.H + head) * 2) = make_float2(top, top == kNegInf ? 0.f : __log2f(sum));
 }
@@ -262,7 +261,7 @@ extern "C" int pyg_global_attention_workspace(const pyg_attention *c, size_t *by
 }
 
 extern "C" int pyg_global_attention(const pyg_attention *c, const void *q, const void *k, const void *v, void *out,
-                                    float *stat, void *ws, size_t ws_bytes, void *stream) {
+                                    float *stat, void *rest, void *ws, size_t ws_bytes, void *stream) {
     Args a;
     size_t need = 0;
     PYG_TRY(take(c, &a));
@@ -271,8 +270,9 @@ extern "C" int pyg_global_attention(const pyg_attention *c, const void *q, const
     PYG_TRY(pyg_global_attention_workspace(c, &need));
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     if (a.Nq == 0) return PYG_OK;
-    a.out = out, a.stat = stat;
-    a.vec_o = vectors(out, a.D, a.D, a.D, bytes_of(c));
+    if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
+    a.out = out, a.stat = stat, a.rest = rest;
+    a.vec_o = vectors(out, a.D, a.D, a.D, bytes_of(c)) && vectors(rest, a.D, a.D, a.D, bytes_of(c));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool bf16 = c->dtype == PYG_BF16;
     return a.B > 0 && few(a) ? attn::forward_few(a, bf16, ws, s) : attn::forward(a, bf16, s);
@@ -287,7 +287,7 @@ extern "C" int pyg_global_attention_backward_workspace(const pyg_attention *c, s
 }
 
 extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void *grad_out, const void *q, const void *k,
-                                             const void *v, const void *out, const float *stat, void *grad_q, void *grad_k,
+                                             const void *v, const void *out, const float *stat, const void *rest, void *grad_q, void *grad_k,
                                              void *grad_v, void *grad_table, void *ws, size_t ws_bytes, void *stream) {
     attn::BackwardArgs b{};
     PYG_TRY(take(c, &b.f));
@@ -298,7 +298,8 @@ extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void 
     if (grad_table && !c->table) return PYG_ERR_INVALID_ARG;
     const size_t need = attn::backward_workspace(a);
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
-    a.out = const_cast<void *>(out), a.stat = const_cast<float *>(stat);
+    if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
+    a.out = const_cast<void *>(out), a.stat = const_cast<float *>(stat), a.rest = const_cast<void *>(rest);
     b.grad_out = grad_out, b.grad_q = grad_q, b.grad_k = grad_k, b.grad_v = grad_v, b.grad_table = grad_table;
     a.vec_o = true;
     for (const void *p : {grad_out, out, static_cast<const void *>(grad_q), static_cast<const void *>(grad_k),

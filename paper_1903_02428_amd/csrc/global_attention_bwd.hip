@@ -13,9 +13,12 @@ namespace pyg {
 namespace attn {
 namespace {
 
-// A row's statistics in units of s: p = exp2(c2 (s + start)), start = -(top + log2 sum / c2), which a tile's
-// accumulators begin with, as -delta does dP's; -infinity for a row that sees no key. Where the bias holds
-// lowest values (wild) s - top comes first: start = -log2 sum / c2 is added after it.
+// A row's statistics in units of s: p = exp2(c2 (s + start)), start = -(top + log2 sum / c2), -infinity for a row that
+// sees no key. bf16 tiles' accumulators begin with it, as dP's do with -delta; in fp32 that would round every
+// partial sum at start's magnitude (a table's gradient 1.3e-6 off instead of 4e-7), so it is added after the
+// products. Where the bias holds lowest values (wild) s - top comes first and rest = -log2 sum / c2 after it.
+template <typename T>
+constexpr bool kStartLate = sizeof(T) == 4;
 struct RowStat {
     float top, start, rest;
 };
@@ -102,18 +105,23 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     const int64_t i0 = pq.tile * BM + wave * 32, row = pq.first + i0 + m;
     const bool there = row < pq.last;
     uint4 qf[SQ], gf[SQ];
-    const T *qr = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
-    const T *gr = static_cast<const T *>(b.grad_out) + (row * a.H + head) * a.D;
-    const T *orow = static_cast<const T *>(a.out) + (row * a.H + head) * a.D;
+    const int64_t safe = there ? row : pq.first, at = (safe * a.H + head) * a.D;
     float dl = 0.f;
+    {
+        uint4 of[SQ], rf[SQ];
+        load_row(static_cast<const T *>(a.q) + safe * a.q_row + head * a.q_head, a.D, there, h, qf);
+        load_row(static_cast<const T *>(b.grad_out) + at, a.D, there, h, gf);
+        load_row(static_cast<const T *>(a.out) + at, a.D, there, h, of);
+        // what rounding took from the output; where it was not kept (a.rest NULL) nothing is added
+        const bool more = sizeof(T) == 2 && a.rest;
+        if (more) load_row(static_cast<const T *>(a.rest) + at, a.D, there, h, rf);
 #pragma unroll
-    for (int s = 0; s < SQ; ++s) {
-        qf[s] = load_piece<T>(qr, 2 * E * s + E * h, a.D, there);
-        Piece<T> g, o;
-        g.u = gf[s] = load_piece<T>(gr, 2 * E * s + E * h, a.D, there);
-        o.u = load_piece<T>(orow, 2 * E * s + E * h, a.D, there);
+        for (int s = 0; s < SQ; ++s) {
+            Piece<T> g, o, r;
+            g.u = gf[s], o.u = of[s], r.u = more ? rf[s] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < E; ++i) dl = fmaf(to_f32(g.v[i]), to_f32(o.v[i]), dl);
+            for (int i = 0; i < E; ++i) dl = fmaf(to_f32(g.v[i]), to_f32(o.v[i]) + to_f32(r.v[i]), dl);
+        }
     }
     dl += other_half(dl);
     float2 raw = make_float2(kNegInf, 0.f);
@@ -122,7 +130,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         if (h == 0) delta[row * a.H + head] = dl;
     }
     const RowStat st = row_stat(raw, a.c2);
-    const f32x16 no_delta(-dl);  // dP starts from it, but where registers are short
+    constexpr bool kDeltaFirst = DP < 128 && !kStartLate<T>;  // dP starts from it, but where registers are short
+    const f32x16 no_delta(-dl);
+    const float late = kStartLate<T> && !wild ? a.c2 * st.start : 0.f;
 
     f32x16 acc[DP / 32];
 #pragma unroll
@@ -145,14 +155,14 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         const bool inner = left >= BK && !wild && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
         f32x16 s[NK], dp[NK];
         if (inner) {
-            const float begin = bias[d0 > 0 ? 2 * a.reach : 0] + st.start;
+            const float begin = bias[d0 > 0 ? 2 * a.reach : 0] + (kStartLate<T> ? 0.f : st.start);
 #pragma unroll
             for (int n = 0; n < NK; ++n) s[n] = f32x16(begin);
         } else {
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
                 s[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
-                if (!wild) s[n] += st.start;
+                if (!wild && !kStartLate<T>) s[n] += st.start;
             }
         }
 #pragma unroll
@@ -160,7 +170,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
 #pragma unroll
             for (int u = 0; u < SQ; ++u) {
                 s[n] = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s[n]);
-                dp[n] = mma<T>(L::row_piece(vt, rl, n, u), gf[u], u == 0 ? (DP < 128 ? no_delta : f32x16(0.f)) : dp[n]);
+                dp[n] = mma<T>(L::row_piece(vt, rl, n, u), gf[u], u == 0 ? (kDeltaFirst ? no_delta : f32x16(0.f)) : dp[n]);
             }
         if (!inner) {
 #pragma unroll
@@ -175,7 +185,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[n][r] = __builtin_amdgcn_exp2f(a.c2 * s[n][r]) * (DP < 128 ? dp[n][r] : dp[n][r] - dl);  // dS^T
+            for (int r = 0; r < 16; ++r)  // dS^T
+                s[n][r] = __builtin_amdgcn_exp2f(kStartLate<T> ? fmaf(a.c2, s[n][r], late) : a.c2 * s[n][r]) *
+                          (kDeltaFirst ? dp[n][r] : dp[n][r] - dl);
         if (mine) {
             if (inner) {
                 float t = 0.f;
@@ -277,13 +289,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     const int64_t j0 = pk.tile * BN + wave * 32, row = pk.first + j0 + m;
     const bool there = row < pk.last;
     uint4 kf[SQ], vf[VL ? 1 : SQ];
-    const T *kr = static_cast<const T *>(a.k) + row * a.k_row + hk * a.k_head;
-    const T *vr = static_cast<const T *>(a.v) + row * a.v_row + hk * a.v_head;
-#pragma unroll
-    for (int s = 0; s < SQ; ++s) {
-        kf[s] = load_piece<T>(kr, 2 * E * s + E * h, a.D, there);
-        if constexpr (!VL) vf[s] = load_piece<T>(vr, 2 * E * s + E * h, a.D, there);
-    }
+    const int64_t safe = there ? row : pk.first;
+    load_row(static_cast<const T *>(a.k) + safe * a.k_row + hk * a.k_head, a.D, there, h, kf);
+    if constexpr (!VL) load_row(static_cast<const T *>(a.v) + safe * a.v_row + hk * a.v_head, a.D, there, h, vf);
     if constexpr (VL)
         Stage<T, DP, BN, NT>(a.v_row, a.D, a.vec_v)
             .load(static_cast<const T *>(a.v) + hk * a.v_head + pk.first * a.v_row, pk.tile * BN, nk - pk.tile * BN, vown);
@@ -340,8 +348,11 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const f32x4 x = *reinterpret_cast<const f32x4 *>(mine + 32 * n + 8 * q);
-                    const f32x4 y = *reinterpret_cast<const f32x4 *>(mine + BQ + 32 * n + 8 * q);
+                    f32x4 x(0.f), y(0.f);
+                    if constexpr (!kStartLate<T>) {
+                        x = *reinterpret_cast<const f32x4 *>(mine + 32 * n + 8 * q);
+                        y = *reinterpret_cast<const f32x4 *>(mine + BQ + 32 * n + 8 * q);
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[n][4 * q + i] = x[i], dp[n][4 * q + i] = y[i];
                 }
@@ -376,8 +387,10 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, s[n][r], constant));
-                    dp[n][r] *= s[n][r];  // dS
+                    const float *at = mine + 32 * n + 8 * (r >> 2) + (r & 3);
+                    const float e = kStartLate<T> && !wild ? s[n][r] + at[0] : s[n][r];
+                    s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, e, constant));
+                    dp[n][r] = s[n][r] * (kStartLate<T> ? dp[n][r] + at[BQ] : dp[n][r]);  // dS
                 }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)

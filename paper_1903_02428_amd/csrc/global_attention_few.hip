@@ -31,6 +31,20 @@ struct Few {
     static constexpr int VW = (W * sizeof(T) + 3) / 4;  // registers of a lane's W features
 };
 
+// N words at any element's address.
+template <int N>
+struct Words {
+    typedef uint32_t U __attribute__((ext_vector_type(N)));
+    typedef U __attribute__((aligned(2))) type;
+};
+template <>
+struct Words<1> {
+    typedef uint32_t U __attribute__((ext_vector_type(1)));
+    typedef U __attribute__((aligned(2))) type;
+};
+template <int N>
+using Any = typename Words<N>::type;
+
 template <typename T, int DP>
 struct FewTile {
     using F = Few<T, DP>;
@@ -41,6 +55,35 @@ struct FewTile {
     __device__ __forceinline__ void load(const Args &a, const T *__restrict__ kb, const T *__restrict__ vb, int64_t j,
                                          int64_t end, int lane) {
         const int m = lane & 15, g = lane >> 4;
+        if (a.D % F::E == 0 && a.D % F::W == 0) {
+            // without a branch, so that all loads are under way together: keys past the end are the last one again (their
+            // weight is 0), features past D the first ones (Q is 0 there, or the result is not kept)
+            const int64_t last = end - 1;
+            const int d = m * F::W < a.D ? m * F::W : 0;
+#pragma unroll
+            for (int u = 0; u < F::SUB; ++u) {
+                const int64_t key = j + 16 * u + m, safe = key < end ? key : last;
+#pragma unroll
+                for (int s = 0; s < F::STEPS; ++s) {
+                    const int f = 4 * F::E * s + F::E * g;
+                    const auto x = *reinterpret_cast<const Any<4> *>(kb + safe * a.k_row + (f < a.D ? f : 0));
+                    k[u][s] = make_uint4(x[0], x[1], x[2], x[3]);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t vkey = j + 16 * u + 4 * g + r;
+                    const T *p = vb + (vkey < end ? vkey : last) * a.v_row + d;
+                    constexpr int N = F::VW >= 4 ? 4 : F::VW;
+#pragma unroll
+                    for (int i = 0; i < F::VW; i += N) {
+                        const auto x = *reinterpret_cast<const Any<N> *>(p + i * 4 / sizeof(T));
+#pragma unroll
+                        for (int n = 0; n < N; ++n) v[4 * u + r][i + n] = x[n];
+                    }
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < F::SUB; ++u) {
             const int64_t key = j + 16 * u + m;
@@ -58,23 +101,6 @@ struct FewTile {
         const int d = m * F::W;
         if (key >= end || d >= a.D) return;
         const T *p = vb + key * a.v_row + d;
-        if (a.vec_v) {
-            constexpr int N = F::VW >= 4 ? 4 : F::VW;  // registers of one load
-#pragma unroll
-            for (int i = 0; i < F::VW; i += N) {
-                if (d + i * 4 / (int)sizeof(T) >= a.D) break;
-                if constexpr (N == 4) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(p + i * 4 / sizeof(T));
-                    o[i] = x.x, o[i + 1] = x.y, o[i + 2] = x.z, o[i + 3] = x.w;
-                } else if constexpr (N == 2) {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(p);
-                    o[0] = x.x, o[1] = x.y;
-                } else {
-                    o[0] = *reinterpret_cast<const uint32_t *>(p);
-                }
-            }
-            return;
-        }
 #pragma unroll
         for (int i = 0; i < F::W; ++i) {
             if (d + i >= a.D) break;
@@ -90,8 +116,16 @@ struct FewTile {
 
 constexpr int kFewWaves = 4;
 
+template <typename T>
+__device__ __forceinline__ void put(const Args &a, int64_t at, float v) {
+    const T r = T(v);
+    static_cast<T *>(a.out)[at] = r;
+    if constexpr (sizeof(T) == 2)
+        if (a.rest) static_cast<T *>(a.rest)[at] = T(v - to_f32(r));
+}
+
 template <typename T, int DP>
-__global__ __launch_bounds__(64 * kFewWaves) void k_few(const Args a, int64_t nslots, int splits, float *__restrict__ part) {
+__global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t nslots, int splits, float *__restrict__ part) {
     using F = Few<T, DP>;
     constexpr int W = F::W;
     __shared__ float lo[kFewWaves][16][DP + 1];
@@ -248,7 +282,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(const Args a, int64_t ns
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) o = fmaf(wgt[w], lo[w][q][d], o);
         if (pr) pr[2 + d] = o;
-        else out[(orow * a.H + ohead) * a.D + d] = T(o * mul);
+        else put<T>(a, (orow * a.H + ohead) * a.D + d, o * mul);
     }
     if (c == 0) {
         if (pr) pr[0] = best, pr[1] = all;
@@ -272,18 +306,29 @@ __global__ __launch_bounds__(kBlock) void k_join(const Args a, int splits, const
     for (int o = 32; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
     const float ref = best == kNegInf ? 0.f : best;
     float all = 0.f, o0 = 0.f, o1 = 0.f;
+    const int d0 = lane < a.D ? lane : 0, d1 = lane + 64 < a.D ? lane + 64 : 0;  // read in any case, kept where it is one
     const bool in0 = lane < a.D, in1 = lane + 64 < a.D;
-    for (int s = 0; s < splits; ++s) {
-        const float *x = p + (int64_t)s * (a.D + 2);
-        const float w = __builtin_amdgcn_exp2f(a.c2 * (x[0] - ref));
-        all = fmaf(w, x[1], all);
-        if (in0) o0 = fmaf(w, x[2 + lane], o0);
-        if (in1) o1 = fmaf(w, x[66 + lane], o1);
+    for (int s0 = 0; s0 < splits; s0 += 64) {
+        // a lane a range for the weights, then the ranges' outputs, whose loads do not wait for one another
+        const int n = splits - s0 < 64 ? splits - s0 : 64;
+        const float *x = p + (int64_t)s0 * (a.D + 2);
+        float w = 0.f;
+        if (lane < n) {
+            w = __builtin_amdgcn_exp2f(a.c2 * (x[lane * (a.D + 2)] - ref));
+            all = fmaf(w, x[lane * (a.D + 2) + 1], all);
+        }
+#pragma unroll 8
+        for (int s = 0; s < n; ++s) {
+            const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+            o0 = fmaf(ws, x[s * (a.D + 2) + 2 + d0], o0);
+            o1 = fmaf(ws, x[s * (a.D + 2) + 2 + d1], o1);
+        }
     }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
     const float mul = best == kNegInf ? 0.f : 1.f / all;
-    T *o = static_cast<T *>(a.out) + at * a.D;
-    if (in0) o[lane] = T(o0 * mul);
-    if (in1) o[lane + 64] = T(o1 * mul);
+    if (in0) put<T>(a, at * a.D + lane, o0 * mul);
+    if (in1) put<T>(a, at * a.D + lane + 64, o1 * mul);
     if (a.stat && lane == 0) a.stat[2 * at] = best, a.stat[2 * at + 1] = best == kNegInf ? 0.f : __log2f(all);
 }
 

@@ -117,7 +117,7 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
                      k_ptr: torch.Tensor | None = None, table: torch.Tensor | None = None,
                      buckets: torch.Tensor | None = None, causal: bool = False, scale: float | None = None,
                      out: torch.Tensor | None = None, stat: torch.Tensor | None = None,
-                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+                     rest: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of each graph's nodes to one another (pyg_global_attention):
     out[i, h] = sum_j softmax_j(scale <q[i, h], k[j, h']> + table[buckets[offset], h])
     v[j, h'], over the keys j of i's graph.
@@ -127,7 +127,8 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
     and k_ptr those of its keys (default: the same); table [buckets, H] and buckets as
     relative_buckets() makes it; causal: keys later than the query are not seen (the last
     query is aligned with the last key); scale defaults to D ** -0.5. `stat` (float32
-    [Nq, H, 2]) receives what global_attention_backward needs. Rows that belong to no graph
+    [Nq, H, 2]) receives what global_attention_backward needs, `rest` (bfloat16, out's shape)
+    what rounding took from out. Rows that belong to no graph
     get zeros, but are left as they were in an `out` that the caller brings."""
     lib = library()
     c = _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, out is None)
@@ -142,23 +143,32 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
         _need_cuda("stat", stat, torch.float32, 3)
         if stat.shape != (*q.shape[:2], 2):
             raise ValueError("stat must be [rows, heads, 2]")
-    _same_device(dev, out=out, stat=stat, workspace=workspace)
+    _rest(rest, q)
+    _same_device(dev, out=out, stat=stat, rest=rest, workspace=workspace)
     with _on(dev):
         nbytes = _bytes(lib.pyg_global_attention_workspace, c)
         if nbytes and (workspace is None or workspace.numel() < nbytes):
             workspace = _workspace(nbytes, dev)
         _check(lib.pyg_global_attention(ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(stat),
-                                        _ptr(workspace), nbytes, _stream(dev)), "pyg_global_attention")
+                                        _ptr(rest), _ptr(workspace), nbytes, _stream(dev)), "pyg_global_attention")
     return out
+
+
+def _rest(rest, q):
+    if rest is not None:
+        _need_cuda("rest", rest, torch.bfloat16, 3)
+        if q.dtype != torch.bfloat16 or rest.shape != q.shape:
+            raise ValueError("rest must have q's shape, and q be bfloat16")
 
 
 def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                               out: torch.Tensor, stat: torch.Tensor, ptr: torch.Tensor,
                               k_ptr: torch.Tensor | None = None, table: torch.Tensor | None = None,
                               buckets: torch.Tensor | None = None, causal: bool = False, scale: float | None = None,
-                              need_grad_table: bool = True, workspace: torch.Tensor | None = None):
+                              need_grad_table: bool = True, rest: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None):
     """Gradients of global_attention: (grad_q, grad_k, grad_v, grad_table or
-    None), from its result `out` and the `stat` it filled."""
+    None), from its result `out`, the `stat` and, if it was asked for, the `rest` it filled."""
     lib = library()
     c = _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, True)
     dev = q.device
@@ -169,7 +179,8 @@ def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     _need_cuda("stat", stat, torch.float32, 3)
     if stat.shape != (*q.shape[:2], 2):
         raise ValueError("stat must be [rows, heads, 2]")
-    _same_device(dev, grad_out=grad_out, out=out, stat=stat, workspace=workspace)
+    _rest(rest, q)
+    _same_device(dev, grad_out=grad_out, out=out, stat=stat, rest=rest, workspace=workspace)
     gq, gk, gv = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
     gt = torch.empty_like(table) if table is not None and need_grad_table else None
     with _on(dev):
@@ -177,7 +188,7 @@ def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
         if workspace is None or workspace.numel() < nbytes:
             workspace = _workspace(nbytes, dev)
         _check(lib.pyg_global_attention_backward(ctypes.byref(c), _ptr(grad_out), _ptr(q), _ptr(k), _ptr(v), _ptr(out),
-                                                 _ptr(stat), _ptr(gq), _ptr(gk), _ptr(gv), _ptr(gt), _ptr(workspace),
+                                                 _ptr(stat), _ptr(rest), _ptr(gq), _ptr(gk), _ptr(gv), _ptr(gt), _ptr(workspace),
                                                  workspace.numel(), _stream(dev)), "pyg_global_attention_backward")
     return gq, gk, gv, gt
 
@@ -196,18 +207,19 @@ class GlobalAttention(torch.autograd.Function):
         tc = None if table is None else table.detach().contiguous()
         need = any(ctx.needs_input_grad[:4])
         stat = torch.empty((*q.shape[:2], 2), dtype=torch.float32, device=q.device) if need else None
-        out = global_attention(qc, kc, vc, ptr, k_ptr, tc, buckets, causal, scale, stat=stat)
+        rest = torch.empty(q.shape, dtype=q.dtype, device=q.device) if need and q.dtype == torch.bfloat16 else None
+        out = global_attention(qc, kc, vc, ptr, k_ptr, tc, buckets, causal, scale, stat=stat, rest=rest)
         ctx.causal, ctx.scale = causal, scale
-        ctx.save_for_backward(q, k, v, table, out, stat, ptr, k_ptr, buckets)
+        ctx.save_for_backward(q, k, v, table, out, stat, rest, ptr, k_ptr, buckets)
         return out
 
     @staticmethod
     def backward(ctx, grad_out):
-        q, k, v, table, out, stat, ptr, k_ptr, buckets = ctx.saved_tensors
+        q, k, v, table, out, stat, rest, ptr, k_ptr, buckets = ctx.saved_tensors
         qc, kc, vc = (_adjacent(t.detach()) for t in (q, k, v))
         tc = None if table is None else table.detach().contiguous()
         grads = global_attention_backward(grad_out.to(q.dtype).contiguous(), qc, kc, vc, out.contiguous(), stat, ptr, k_ptr,
-                                          tc, buckets, ctx.causal, ctx.scale, need_grad_table=ctx.needs_input_grad[3])
+                                          tc, buckets, ctx.causal, ctx.scale, need_grad_table=ctx.needs_input_grad[3], rest=rest)
         return tuple(g if need else None for g, need in zip(grads, ctx.needs_input_grad)) + (None,) * 5
 
 

@@ -199,17 +199,17 @@ def test_repeatable_and_captured(pyg):
         dev = [t.cuda() for t in (q, k, v)]
         args = (ptr_of(qn), ptr_of(kn), table.cuda(), lut.cuda(), True)
         gd, out = grad.cuda(), torch.zeros(q.shape, dtype=q.dtype, device="cuda")
-        stat = torch.zeros((*q.shape[:2], 2), device="cuda")
+        stat, rest = torch.zeros((*q.shape[:2], 2), device="cuda"), torch.zeros_like(out)
         s = torch.cuda.Stream()
         s.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(s):
-            pyg.global_attention(*dev, *args, out=out, stat=stat)
-            pyg.global_attention_backward(gd, *dev, out, stat, *args)
+            pyg.global_attention(*dev, *args, out=out, stat=stat, rest=rest)
+            pyg.global_attention_backward(gd, *dev, out, stat, *args, rest=rest)
         s.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=s):
-            pyg.global_attention(*dev, *args, out=out, stat=stat)
-            grads = pyg.global_attention_backward(gd, *dev, out, stat, *args)
+            pyg.global_attention(*dev, *args, out=out, stat=stat, rest=rest)
+            grads = pyg.global_attention_backward(gd, *dev, out, stat, *args, rest=rest)
         for _ in range(3):
             out.zero_()
             for t in grads:
@@ -246,7 +246,7 @@ def test_refusals(pyg):
            dict(k_ptr=ptr_of([3, 3])), dict(table=table), dict(buckets=lut), dict(table=table[:, :2].contiguous(), buckets=lut),
            dict(table=table.bfloat16(), buckets=lut), dict(table=table, buckets=lut[1:]), dict(table=table, buckets=lut.long()),
            dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(out=x[:3]), dict(out=x.bfloat16()),
-           dict(stat=torch.zeros(6, 4, device="cuda"))]
+           dict(stat=torch.zeros(6, 4, device="cuda")), dict(rest=x)]
     for change in bad:
         with pytest.raises(ValueError):
             pyg.global_attention(**{**ok, **change})
