@@ -42,7 +42,7 @@ __device__ __forceinline__ float to_f32(__bf16 v) { return static_cast<float>(v)
 // rounding (tables of lowest values): s - m has to come first then.
 constexpr float kWild = 65536.f;
 template <typename T>
-__device__ __forceinline__ bool stage_bias(const Args &a, int h, float *bias) {
+__device__ __forceinline__ bool stage_bias(const Args &a, int h, float *bias, int *buckets = nullptr) {
     int wild = 0;
     const T *t = static_cast<const T *>(a.table);
     for (int o = threadIdx.x; o <= 2 * a.reach; o += blockDim.x) {
@@ -50,6 +50,7 @@ __device__ __forceinline__ bool stage_bias(const Args &a, int h, float *bias) {
         if (t) {
             int b = a.lut[o];
             b = b < 0 ? 0 : b >= a.buckets ? a.buckets - 1 : b;
+            if (buckets) buckets[o] = b;
             const float raw = to_f32(t[(int64_t)b * a.H + h]);
             v = raw * a.inv_scale;
             if (fabsf(raw) <= -kLowest) v = fminf(fmaxf(v, kLowest), -kLowest);

@@ -70,6 +70,13 @@ __device__ __forceinline__ f32x16 mma(uint4 a, uint4 b, f32x16 c) {
     }
 }
 
+// Whether piece s of a row holds nothing but padding: skipped where a product takes
+// long (fp32: 256 cycles a piece); elsewhere the test costs more than it saves.
+template <typename T>
+__device__ __forceinline__ bool past(int s, int D) {
+    return sizeof(T) == 4 && 2 * Elem<T>::E * s >= D;
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const bf16x2 p = __builtin_convertvector(f32x2{a, b}, bf16x2);  // one rounding to nearest even, NaN kept
     return __builtin_bit_cast(uint32_t, p);

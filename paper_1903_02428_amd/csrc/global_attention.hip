@@ -20,8 +20,9 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
     constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
     using L = Tile<T, DP>;
     constexpr int kTile = L::template bytes<BK>();
-    extern __shared__ __align__(16) char lds[];  // K and V of two tiles, the bias
-    float *bias = reinterpret_cast<float *>(lds + 4 * kTile);
+    constexpr int HALVES = WAVES == 1 ? 1 : 2;   // a lone wavefront's graphs are mostly one tile: others hide its waits
+    extern __shared__ __align__(16) char lds[];  // K and V of one or two tiles, the bias
+    float *bias = reinterpret_cast<float *>(lds + 2 * HALVES * kTile);
     const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     // key heads vary fastest: with up to 8 of them (or a multiple) every XCD's L2 sees its own heads' keys only
     const uint32_t id = blockIdx.x;
@@ -35,7 +36,6 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         if (a.zero_rest) zero_rows(out, q0, q0 + BM < pq.last ? q0 + BM : pq.last, a.H, head, a.D);
         return;
     }
-    const bool wild = stage_bias<T>(a, head, bias);
     const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
                   k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
     const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
@@ -45,9 +45,6 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
     const int64_t i0 = pq.tile * BM + wave * 32;  // first query of the wavefront, in the graph
     const int64_t row = pq.first + i0 + m;        // the lane's query row
     const bool there = row < pq.last;
-    uint4 qf[SQ];
-    load_row(static_cast<const T *>(a.q) + (there ? row : pq.first) * a.q_row + head * a.q_head, a.D, there, h, qf);
-
     f32x16 acc[DP / 32];
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) acc[t] = f32x16(0.f);
@@ -59,6 +56,17 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
     }
     const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
+    auto fetch = [&](int64_t j0, int half) {
+        if (j0 >= end) return;
+        sk.load(kb, j0, nk - j0, lds + 2 * half * kTile);
+        sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
+    };
+    // the bias, the first tile and the queries wait for memory together
+    uint4 qf[SQ];
+    fetch(0, 0);
+    const bool wild = stage_bias<T>(a, head, bias);
+    load_row(static_cast<const T *>(a.q) + (there ? row : pq.first) * a.q_row + head * a.q_head, a.D, there, h, qf);
+    registers_loaded();
     const typename L::RowLane rl(lane);
     const typename L::ColLane cl(lane);
     const int64_t shift = i0 + nk - nq;  // offset of key j and the wavefront's first query: j - shift
@@ -78,7 +86,10 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int s = 0; s < SQ; ++s) st[n] = mma<T>(L::row_piece(kt, rl, n, s), qf[s], st[n]);
+            for (int s = 0; s < SQ; ++s) {
+                if (past<T>(s, a.D)) break;
+                st[n] = mma<T>(L::row_piece(kt, rl, n, s), qf[s], st[n]);
+            }
         if (!inner) {
 #pragma unroll
             for (int n = 0; n < NK; ++n) mask_tile<true>(st[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
@@ -123,24 +134,29 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
                 for (int d = 0; d < DP / 32; ++d) acc[d] = mma<T>(L::col_piece(vt, cl, n, d, u), p, acc[d]);
             }
     };
-    // the next tile is on its way to one half of the LDS while the other is worked on
-    auto fetch = [&](int64_t j0, int half) {
-        if (j0 >= end) return;
-        sk.load(kb, j0, nk - j0, lds + 2 * half * kTile);
-        sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
-    };
-    registers_loaded();
-    fetch(0, 0);
-    for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
-        loads_done();
-        __syncthreads();  // the tile is there, and nobody reads the other half any more
-        fetch(j0 + BK, 1);
-        step(lds, lds + kTile, j0);
-        if (j0 + BK >= end) break;
-        loads_done();
-        __syncthreads();
-        fetch(j0 + 2 * BK, 0);
-        step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
+    if constexpr (HALVES == 1) {
+        for (int64_t j0 = 0; j0 < end; j0 += BK) {
+            if (j0 > 0) {
+                __syncthreads();
+                fetch(j0, 0);
+            }
+            loads_done();
+            __syncthreads();
+            step(lds, lds + kTile, j0);
+        }
+    } else {
+        // the next tile is on its way to one half of the LDS while the other is worked on
+        for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
+            loads_done();
+            __syncthreads();  // the tile is there, and nobody reads the other half any more
+            fetch(j0 + BK, 1);
+            step(lds, lds + kTile, j0);
+            if (j0 + BK >= end) break;
+            loads_done();
+            __syncthreads();
+            fetch(j0 + 2 * BK, 0);
+            step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
+        }
     }
     sum += other_half(sum);
     const float mul = top == kNegInf ? 0.f : 1.f / sum;
@@ -154,7 +170,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
 template <typename T, int DP, int WAVES, int BK>
 int launch(const Args &a, hipStream_t s) {
     const int64_t n = slots(a.Nq, a.B, 32 * WAVES);
-    const size_t bytes = 4 * Tile<T, DP>::template bytes<BK>() + (2 * a.reach + 1) * sizeof(float);
+    const size_t bytes = (WAVES == 1 ? 2 : 4) * Tile<T, DP>::template bytes<BK>() + (2 * a.reach + 1) * sizeof(float);
     if (n * a.H >= (int64_t(1) << 32) / (64 * WAVES)) return PYG_ERR_UNSUPPORTED;
     k_forward<T, DP, WAVES, BK><<<static_cast<unsigned>(n * a.H), 64 * WAVES, bytes, s>>>(a, n);
     PYG_LAUNCH_CHECK();

@@ -74,8 +74,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
     using L = Tile<T, DP>;
     constexpr int kTile = L::template bytes<BK>();
-    extern __shared__ __align__(16) char lds[];  // K and V of two tiles, the bias, the sums by offset
-    float *bias = reinterpret_cast<float *>(lds + 4 * kTile);
+    constexpr int HALVES = WAVES == 1 ? 1 : 2;
+    extern __shared__ __align__(16) char lds[];  // K and V of one or two tiles, the bias, the sums by offset
+    float *bias = reinterpret_cast<float *>(lds + 2 * HALVES * kTile);
     float *hist = bias + (2 * a.reach + 1);  // a wavefront's own sums by offset
     const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     const uint32_t id = blockIdx.x;
@@ -94,8 +95,8 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     const int offsets = 2 * a.reach + 1;
     if (mine)
         for (int i = threadIdx.x; i < offsets * WAVES; i += NT) hist[i] = 0.f;
-    const bool wild = stage_bias<T>(a, head, bias);
     float *own = hist + wave * offsets, *skew = hist + WAVES * offsets + wave * kSkew;
+    int *bucket = reinterpret_cast<int *>(hist + WAVES * (offsets + kSkew));  // of every offset
     const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)),
                   k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
     const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = pq.last - pq.first;
@@ -105,6 +106,20 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     const int64_t i0 = pq.tile * BM + wave * 32, row = pq.first + i0 + m;
     const bool there = row < pq.last;
     uint4 qf[SQ], gf[SQ];
+    int64_t end = nk;
+    if (a.causal) {
+        const int64_t seen = pq.tile * BM + BM + nk - nq;
+        end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
+    }
+    const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
+    auto fetch = [&](int64_t j0, int half) {
+        if (j0 >= end) return;
+        sk.load(kb, j0, nk - j0, lds + 2 * half * kTile);
+        sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
+    };
+    // the first tile, the bias and the queries' rows wait for memory together
+    fetch(0, 0);
+    const bool wild = stage_bias<T>(a, head, bias, mine ? bucket : nullptr);
     const int64_t safe = there ? row : pq.first, at = (safe * a.H + head) * a.D;
     float dl = 0.f;
     {
@@ -134,17 +149,12 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     const f32x16 no_delta(-dl);
     const float late = kStartLate<T> && !wild ? a.c2 * st.start : 0.f;
 
+    registers_loaded();
     f32x16 acc[DP / 32];
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) acc[t] = f32x16(0.f);
     float below = 0.f, above = 0.f;  // the lane's dS of whole tiles beyond the reach
 
-    int64_t end = nk;
-    if (a.causal) {
-        const int64_t seen = pq.tile * BM + BM + nk - nq;
-        end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
-    }
-    const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
     const typename L::RowLane rl(lane);
     const typename L::ColLane cl(lane);
     const int64_t shift = i0 + nk - nq;
@@ -169,6 +179,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int u = 0; u < SQ; ++u) {
+                if (past<T>(u, a.D)) break;
                 s[n] = mma<T>(L::row_piece(kt, rl, n, u), qf[u], s[n]);
                 dp[n] = mma<T>(L::row_piece(vt, rl, n, u), gf[u], u == 0 ? (kDeltaFirst ? no_delta : f32x16(0.f)) : dp[n]);
             }
@@ -210,23 +221,28 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
                 for (int t = 0; t < DP / 32; ++t) acc[t] = mma<T>(L::col_piece(kt, cl, n, t, u), p, acc[t]);
             }
     };
-    auto fetch = [&](int64_t j0, int half) {
-        if (j0 >= end) return;
-        sk.load(kb, j0, nk - j0, lds + 2 * half * kTile);
-        sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
-    };
-    registers_loaded();
-    fetch(0, 0);
-    for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
-        loads_done();
-        __syncthreads();
-        fetch(j0 + BK, 1);
-        step(lds, lds + kTile, j0);
-        if (j0 + BK >= end) break;
-        loads_done();
-        __syncthreads();
-        fetch(j0 + 2 * BK, 0);
-        step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
+    if constexpr (HALVES == 1) {
+        for (int64_t j0 = 0; j0 < end; j0 += BK) {
+            if (j0 > 0) {
+                __syncthreads();
+                fetch(j0, 0);
+            }
+            loads_done();
+            __syncthreads();
+            step(lds, lds + kTile, j0);
+        }
+    } else {
+        for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
+            loads_done();
+            __syncthreads();
+            fetch(j0 + BK, 1);
+            step(lds, lds + kTile, j0);
+            if (j0 + BK >= end) break;
+            loads_done();
+            __syncthreads();
+            fetch(j0 + 2 * BK, 0);
+            step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
+        }
     }
     store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
     if (mine) {
@@ -236,10 +252,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         for (int i = threadIdx.x; i < a.buckets; i += NT) {
             float t = 0.f;
             for (int o = 0; o < offsets; ++o) {
-                int l = a.lut[o];
-                l = l < 0 ? 0 : l >= a.buckets ? a.buckets - 1 : l;
-                if (l != i) continue;
-                for (int w = 0; w < WAVES; ++w) t += hist[w * offsets + o];
+                const bool here = bucket[o] == i;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) t += here ? hist[w * offsets + o] : 0.f;
             }
             mine[i] = t;
         }
@@ -258,9 +273,10 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     using L = Tile<T, DP>;
     constexpr int kTile = L::template bytes<BQ>();
     static_assert(BQ <= NT, "a thread a query's statistics");
-    extern __shared__ __align__(16) char lds[];  // Q and dO of two tiles, their statistics, the bias
+    constexpr int HALVES = WAVES == 1 ? 1 : 2;
+    extern __shared__ __align__(16) char lds[];  // Q and dO of one or two tiles, their statistics, the bias
     constexpr bool VL = kValuesInLds<T, DP>;
-    char *vown = lds + 4 * kTile;
+    char *vown = lds + 2 * HALVES * kTile;
     float *stats = reinterpret_cast<float *>(vown + (VL ? L::template bytes<BN>() : 0));  // [2][4][BQ]: start, -delta, top, rest
     float *bias = stats + 8 * BQ;
     const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
@@ -367,6 +383,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int u = 0; u < SQ; ++u) {
+                    if (past<T>(u, a.D)) break;
                     s[n] = mma<T>(L::row_piece(qt, rl, n, u), kf[u], s[n]);
                     dp[n] = mma<T>(L::row_piece(gt, rl, n, u), VL ? L::row_piece(vmine, rl, 0, u) : vf[VL ? 0 : u], dp[n]);
                 }
@@ -405,21 +422,34 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
                 }
         };
         __syncthreads();  // the last head's tiles and bias are done with
+        fetch(begin, 0);
         wild = stage_bias<T>(a, head, bias);
         registers_loaded();
-        fetch(begin, 0);
-        for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
-            put(i0, 0);
-            loads_done();
-            __syncthreads();
-            fetch(i0 + BQ, 1);
-            step(lds, lds + kTile, stats, i0);
-            if (i0 + BQ >= nq) break;
-            put(i0 + BQ, 1);
-            loads_done();
-            __syncthreads();
-            fetch(i0 + 2 * BQ, 0);
-            step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
+        if constexpr (HALVES == 1) {
+            for (int64_t i0 = begin; i0 < nq; i0 += BQ) {
+                if (i0 > begin) {
+                    __syncthreads();
+                    fetch(i0, 0);
+                }
+                put(i0, 0);
+                loads_done();
+                __syncthreads();
+                step(lds, lds + kTile, stats, i0);
+            }
+        } else {
+            for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
+                put(i0, 0);
+                loads_done();
+                __syncthreads();
+                fetch(i0 + BQ, 1);
+                step(lds, lds + kTile, stats, i0);
+                if (i0 + BQ >= nq) break;
+                put(i0 + BQ, 1);
+                loads_done();
+                __syncthreads();
+                fetch(i0 + 2 * BQ, 0);
+                step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
+            }
         }
     }
     if (splits > 1) {
@@ -455,21 +485,22 @@ int kv_splits(const Args &a, int64_t tiles) {
 }
 int64_t key_tiles(const Args &a) { return a.Nk / 128 + 1; }
 
-// dT[b, h] from the workgroups' shares [slots, H, buckets], in a fixed order: 64
-// slots in turn by each of the workgroup's rows of threads, then the rows.
+// dT[b, h] from the workgroups' shares [slots, H, buckets], in a fixed order: every
+// 64th slot by each of the workgroup's 64 rows of threads, then the rows.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_grad_table(const float *__restrict__ part, int64_t nslots, int H, int buckets,
+__global__ __launch_bounds__(1024) void k_grad_table(const float *__restrict__ part, int64_t nslots, int H, int buckets,
                                                        T *__restrict__ out) {
-    __shared__ double sums[kBlock];
+    __shared__ double sums[1024];
     const int head = blockIdx.x, i = threadIdx.x & 15, r = threadIdx.x >> 4;
     const int bk = blockIdx.y * 16 + i;
     double t = 0;
     if (bk < buckets)
-        for (int64_t s = r; s < nslots; s += kBlock / 16) t += part[(s * H + head) * buckets + bk];
+#pragma unroll 8
+        for (int64_t s = r; s < nslots; s += 64) t += part[(s * H + head) * buckets + bk];
     sums[threadIdx.x] = t;
     __syncthreads();
     if (r == 0 && bk < buckets) {
-        for (int k = 1; k < kBlock / 16; ++k) t += sums[16 * k + i];
+        for (int k = 1; k < 64; ++k) t += sums[16 * k + i];
         out[(int64_t)bk * H + head] = T(static_cast<float>(t));
     }
 }
@@ -488,9 +519,9 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     float *part = c.take<float>(b.grad_table ? nq * a.H * a.buckets : 0);
     float *kv_part = c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
     if (!b.grad_table) part = nullptr;
-    const size_t tiles = 4 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
+    const size_t tiles = (WAVES == 1 ? 2 : 4) * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
     k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES,
-                                 tiles + bias * (part ? 1 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(b, nq, delta, part);
+                                 tiles + bias * (part ? 2 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(b, nq, delta, part);
     PYG_LAUNCH_CHECK();
     const size_t own = kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0;
     k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv * splits), 64 * WAVES,
@@ -503,7 +534,7 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
         PYG_LAUNCH_CHECK();
     }
     if (part) {
-        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), kBlock, 0, s>>>(part, nq, a.H, a.buckets,
+        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), 1024, 0, s>>>(part, nq, a.H, a.buckets,
                                                                             static_cast<T *>(b.grad_table));
         PYG_LAUNCH_CHECK();
     }

@@ -317,11 +317,14 @@ __global__ __launch_bounds__(kBlock) void k_join(const Args a, int splits, const
             w = __builtin_amdgcn_exp2f(a.c2 * (x[lane * (a.D + 2)] - ref));
             all = fmaf(w, x[lane * (a.D + 2) + 1], all);
         }
-#pragma unroll 8
-        for (int s = 0; s < n; ++s) {
-            const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
-            o0 = fmaf(ws, x[s * (a.D + 2) + 2 + d0], o0);
-            o1 = fmaf(ws, x[s * (a.D + 2) + 2 + d1], o1);
+        for (int s = 0; s < n; s += 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {  // past the last range the weight is 0
+                const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s + i));
+                const float *o = x + (s + i < n ? s + i : n - 1) * (a.D + 2) + 2;
+                o0 = fmaf(ws, o[d0], o0);
+                o1 = fmaf(ws, o[d1], o1);
+            }
         }
     }
 #pragma unroll
