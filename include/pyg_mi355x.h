@@ -760,7 +760,7 @@ int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
  * weights p are rounded to bf16 for the second product. Deterministic.
  * Errors: PYG_ERR_INVALID_ARG (NULL or negative or inconsistent arguments,
  * Hkv not dividing H, scale not in (0, 1e30], overlapping strides),
- * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 4096, rows >= 2^31, a grid
+ * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 1024, rows >= 2^31, a grid
  * beyond 2^32 threads), PYG_ERR_WORKSPACE. */
 int pyg_global_attention(const pyg_attention *a, const void *q, const void *k, const void *v, void *out, float *stat,
                          void *rest, void *ws, size_t ws_bytes, void *stream);

@@ -29,7 +29,7 @@ struct Args {
     float *stat;  // [Nq, H, 2]: the row's largest s, log2 of its sum of exp2(c2 (s - m)); or NULL
 };
 
-constexpr int kMaxReach = 4096;
+constexpr int kMaxReach = 1024;  // the sums by offset of four wavefronts fit the LDS beside the widest tiles
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__bf16 v) { return static_cast<float>(v); }

@@ -273,10 +273,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
     using L = Tile<T, DP>;
     constexpr int kTile = L::template bytes<BQ>();
     static_assert(BQ <= NT, "a thread a query's statistics");
-    constexpr int HALVES = WAVES == 1 ? 1 : 2;
-    extern __shared__ __align__(16) char lds[];  // Q and dO of one or two tiles, their statistics, the bias
+    extern __shared__ __align__(16) char lds[];  // Q and dO of two tiles, their statistics, the bias
     constexpr bool VL = kValuesInLds<T, DP>;
-    char *vown = lds + 2 * HALVES * kTile;
+    char *vown = lds + 4 * kTile;
     float *stats = reinterpret_cast<float *>(vown + (VL ? L::template bytes<BN>() : 0));  // [2][4][BQ]: start, -delta, top, rest
     float *bias = stats + 8 * BQ;
     const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
@@ -425,31 +424,18 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
         fetch(begin, 0);
         wild = stage_bias<T>(a, head, bias);
         registers_loaded();
-        if constexpr (HALVES == 1) {
-            for (int64_t i0 = begin; i0 < nq; i0 += BQ) {
-                if (i0 > begin) {
-                    __syncthreads();
-                    fetch(i0, 0);
-                }
-                put(i0, 0);
-                loads_done();
-                __syncthreads();
-                step(lds, lds + kTile, stats, i0);
-            }
-        } else {
-            for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
-                put(i0, 0);
-                loads_done();
-                __syncthreads();
-                fetch(i0 + BQ, 1);
-                step(lds, lds + kTile, stats, i0);
-                if (i0 + BQ >= nq) break;
-                put(i0 + BQ, 1);
-                loads_done();
-                __syncthreads();
-                fetch(i0 + 2 * BQ, 0);
-                step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
-            }
+        for (int64_t i0 = begin; i0 < nq; i0 += 2 * BQ) {
+            put(i0, 0);
+            loads_done();
+            __syncthreads();
+            fetch(i0 + BQ, 1);
+            step(lds, lds + kTile, stats, i0);
+            if (i0 + BQ >= nq) break;
+            put(i0 + BQ, 1);
+            loads_done();
+            __syncthreads();
+            fetch(i0 + 2 * BQ, 0);
+            step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
         }
     }
     if (splits > 1) {
@@ -519,13 +505,13 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     float *part = c.take<float>(b.grad_table ? nq * a.H * a.buckets : 0);
     float *kv_part = c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
     if (!b.grad_table) part = nullptr;
-    const size_t tiles = (WAVES == 1 ? 2 : 4) * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
+    const size_t pair = 2 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
     k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES,
-                                 tiles + bias * (part ? 2 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(b, nq, delta, part);
+                                 pair * (WAVES == 1 ? 1 : 2) + bias * (part ? 2 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(b, nq, delta, part);
     PYG_LAUNCH_CHECK();
     const size_t own = kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0;
     k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv * splits), 64 * WAVES,
-                                  tiles + own + 8 * BK * sizeof(float) + bias, s>>>(b, nk, delta, splits, kv_part);
+                                  2 * pair + own + 8 * BK * sizeof(float) + bias, s>>>(b, nk, delta, splits, kv_part);
     PYG_LAUNCH_CHECK();
     if (splits > 1) {
         const int64_t n = a.Nk * a.Hkv * a.D;

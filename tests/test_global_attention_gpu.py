@@ -69,6 +69,10 @@ CASES = [
     ([700], [257], 2, 2, 32, 8, 16, True),
     ([130, 250], None, 3, 1, 7, 2, 1, False),
     ([190], [333], 1, 1, 1, 0, 0, False),
+    # the largest reach and the most buckets, beside the widest heads
+    ([140, 20], None, 1, 1, 128, 1024, 1024, False),
+    ([30, 20], None, 1, 1, 128, 1024, 1024, True),
+    ([1, 2], [40, 1500], 2, 1, 128, 1024, 1024, True),
     # heads of a group dealt out over workgroups (few key tiles): all of them, and a part
     ([150, 140], None, 6, 1, 40, 8, 16, True),
     ([260], [140], 8, 2, 64, 4, 8, False),
@@ -255,6 +259,9 @@ def test_refusals(pyg):
     wide = torch.zeros(6, 1, 129, device="cuda")
     with pytest.raises(pyg.PygError):
         pyg.global_attention(wide, wide, wide, ptr)
+    far = torch.zeros(2 * 1025 + 1, dtype=torch.int32, device="cuda")
+    with pytest.raises(pyg.PygError):
+        pyg.global_attention(x, x, x, ptr, None, table, far)
     same = x[:1].expand(6, 4, 8)  # one row six times: rows overlap
     with pytest.raises(pyg.PygError):
         pyg.global_attention(x, same, same, ptr)
