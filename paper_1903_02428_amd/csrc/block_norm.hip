@@ -4,7 +4,7 @@
 // (rms); each part may be left out.
 //
 // Bound by memory: every input is read once and r and y written once, a row
-// staying in registers between. L lanes share a row (a 16-lane group, a
+// staying in registers between. L lanes share a row (8 to 64 of them, a
 // wavefront or a workgroup, by its width), a lane holding NV pieces of 16 bytes;
 // means and variances are fp32 and two-pass (the deviations from the mean are
 // squared). The backward reads the same inputs and the two gradients, makes the
@@ -24,12 +24,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 
-template <typename T, int NV>
-struct Row {
-    static constexpr int E = 16 / sizeof(T);
-    float v[NV * E];
-};
-
 template <typename T>
 __device__ __forceinline__ void unpack16(const u32x4 &u, float *v) {
     if constexpr (sizeof(T) == 4) {
@@ -48,17 +42,23 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// One piece of a row from feature f on: zeros past F.
+// One piece of a row from feature f on, as it lies in memory: zeros past F.
 template <typename T>
-__device__ __forceinline__ void load_piece(const T *__restrict__ row, int f, int F, float *v) {
+__device__ __forceinline__ u32x4 load_piece(const T *__restrict__ row, int f, int F) {
     constexpr int E = 16 / sizeof(T);
-    if (f + E <= F) {
-        const u32x4 u = *reinterpret_cast<const u32x4_any *>(row + f);
-        unpack16<T>(u, v);
-        return;
+    if (f + E <= F) return *reinterpret_cast<const u32x4_any *>(row + f);
+    u32x4 u{0, 0, 0, 0};
+    if (f < F) {  // the last piece of a row whose width is no multiple
+        uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+        for (int i = 0; f + i < F; ++i) {
+            const uint64_t b = sizeof(T) == 4 ? reinterpret_cast<const uint32_t *>(row)[f + i]
+                                              : reinterpret_cast<const uint16_t *>(row)[f + i];
+            (i < E / 2 ? lo : hi) |= b << (8 * sizeof(T) * (i % (E / 2)));
+        }
+        u = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
     }
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = f + i < F ? static_cast<float>(row[f + i]) : 0.f;
+    return u;
 }
 
 template <typename T>
@@ -100,18 +100,39 @@ struct Norm {
     int sums;
 };
 
-// Sums over the L lanes of a row, K at once.
+constexpr int kRowLds = 2 * 16;  // sums of a workgroup's wavefronts
+struct Sums {
+    float *lds;  // [2][kRowLds]
+    int turn = 0;
+};
+
+// Rows within a wavefront share a workgroup of four; a wider row has its own.
+constexpr int threads_of(int L) { return L <= 64 ? 256 : L; }
+
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+
+// Sums over the L lanes of a row, K at once: 16 lanes by moves within the vector unit
+// (neighbours, pairs, then mirrored halves and rows), further ones through LDS.
 template <int L, int K>
-__device__ __forceinline__ void row_sums(float (&v)[K], float *lds) {
-    constexpr int W = L < 64 ? L : 64;
+__device__ __forceinline__ void row_sums(float (&v)[K], Sums &at) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int o = W / 2; o > 0; o >>= 1) v[k] += __shfl_xor(v[k], o);
+    for (int k = 0; k < K; ++k) {
+        v[k] += moved<0xB1>(v[k]);   // quad_perm [1, 0, 3, 2]
+        v[k] += moved<0x4E>(v[k]);   // quad_perm [2, 3, 0, 1]
+        v[k] += moved<0x141>(v[k]);  // row_half_mirror
+        if constexpr (L >= 16) v[k] += moved<0x140>(v[k]);  // row_mirror
+        if constexpr (L >= 32) v[k] += __shfl_xor(v[k], 16);
+        if constexpr (L >= 64) v[k] += __shfl_xor(v[k], 32);
+    }
     if constexpr (L > 64) {
         constexpr int waves = L / 64;
         const int wave = threadIdx.x >> 6;
-        __syncthreads();
+        // two halves in turn: who writes one has passed the barrier after which all had read it
+        float *lds = at.lds + at.turn * kRowLds;
+        at.turn ^= 1;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int k = 0; k < K; ++k) lds[k * waves + wave] = v[k];
@@ -129,10 +150,17 @@ template <typename T, int L, int NV>
 struct Body {
     static constexpr int E = 16 / sizeof(T), M = NV * E;
     static __device__ __forceinline__ int feature(int lane, int i) { return (lane + L * i) * E; }
-    static __device__ __forceinline__ void load(const void *p, int64_t row, int F, int lane, float (&v)[M]) {
+    struct Raw {
+        u32x4 u[NV];
+    };
+    static __device__ __forceinline__ void fetch(const void *p, int64_t row, int F, int lane, Raw &r) {
         const T *x = static_cast<const T *>(p) + row * F;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) load_piece<T>(x, feature(lane, i), F, v + i * E);
+        for (int i = 0; i < NV; ++i) r.u[i] = load_piece<T>(x, feature(lane, i), F);
+    }
+    static __device__ __forceinline__ void open(const Raw &r, float (&v)[M]) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) unpack16<T>(r.u[i], v + i * E);
     }
     static __device__ __forceinline__ void store(void *p, int64_t row, int F, int lane, const float (&v)[M]) {
         T *x = static_cast<T *>(p) + row * F;
@@ -142,17 +170,17 @@ struct Body {
     // a [F] parameter in fp32, `other` where it is missing
     static __device__ __forceinline__ void load_param(const float *p, int F, int lane, float other, float (&v)[M]) {
 #pragma unroll
+        for (int k = 0; k < M; ++k) v[k] = other;
+        if (!p) return;
+#pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int f = feature(lane, i) + e;
-                v[i * E + e] = !p ? other : f < F ? p[f] : 0.f;
-            }
+            for (int e = 0; e < E; e += 4) unpack16<float>(load_piece<float>(p, feature(lane, i) + e, F), v + i * E + e);
     }
     static __device__ __forceinline__ bool inside(int lane, int k, int F) { return feature(lane, k / E) + k % E < F; }
 
     // x -> its normalised values; returns 1 / deviation
-    static __device__ __forceinline__ float normalise(float (&x)[M], const Norm &a, int lane, float *lds) {
+    static __device__ __forceinline__ float normalise(float (&x)[M], const Norm &a, int lane, Sums &lds) {
         if (a.layer) {
             float s[1] = {0.f};
 #pragma unroll
@@ -166,14 +194,14 @@ struct Body {
 #pragma unroll
         for (int k = 0; k < M; ++k) q[0] = fmaf(x[k], x[k], q[0]);
         row_sums<L, 1>(q, lds);
-        const float rstd = 1.f / sqrtf(fmaf(q[0], a.inv_F, a.eps));
+        const float rstd = __builtin_amdgcn_rsqf(fmaf(q[0], a.inv_F, a.eps));  // within one step of fp32
 #pragma unroll
         for (int k = 0; k < M; ++k) x[k] *= rstd;
         return rstd;
     }
     // gradient t of the normalised values n -> gradient of x
     static __device__ __forceinline__ void through(float (&t)[M], const float (&n)[M], float rstd, const Norm &a, int lane,
-                                                   float *lds) {
+                                                   Sums &lds) {
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < M; ++k) s[0] = fmaf(t[k], n[k], s[0]), s[1] += t[k];
@@ -184,15 +212,17 @@ struct Body {
     }
 };
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
-
-constexpr int kRowLds = 2 * 16;  // sums of a workgroup's wavefronts
+// exp and reciprocal by the hardware's instructions, each within one step of fp32 (and the exponent's rounding)
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x));
+}
 
 template <typename T, int L, int NV>
-__global__ __launch_bounds__(L < 256 ? 256 : L) void k_block_norm(const Norm a) {
+__global__ __launch_bounds__(threads_of(L)) void k_block_norm(const Norm a) {
     using B = Body<T, L, NV>;
-    constexpr int M = B::M, E = B::E, R = (L < 256 ? 256 : L) / L;
-    __shared__ float lds[kRowLds];
+    constexpr int M = B::M, E = B::E, R = threads_of(L) / L;
+    __shared__ float sums_lds[2 * kRowLds];
+    Sums lds{sums_lds};
     const int lane = threadIdx.x % L;
     float sc[M], pw[M], pb[M], w[M], b[M];
     B::load_param(a.scale, a.F, lane, 1.f, sc);
@@ -200,13 +230,23 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void k_block_norm(const Norm a) 
     B::load_param(a.post_b, a.F, lane, 0.f, pb);
     B::load_param(a.w, a.F, lane, 1.f, w);
     B::load_param(a.b, a.F, lane, 0.f, b);
-    for (int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L; row < a.N; row += (int64_t)gridDim.x * R) {
+    const int64_t step = (int64_t)gridDim.x * R;
+    int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+    typename B::Raw rh, rr, rg;
+    auto fetch = [&](int64_t at) {
+        B::fetch(a.h, at, a.F, lane, rh);
+        if (a.residual) B::fetch(a.residual, at, a.F, lane, rr);
+        if (a.gate && !a.gate_rows) B::fetch(a.gate, at, a.F, lane, rg);
+    };
+    if (row < a.N) fetch(row);
+    for (; row < a.N; row += step) {
         float x[M], res[M], g[M];
-        B::load(a.h, row, a.F, lane, x);
-        if (a.residual) B::load(a.residual, row, a.F, lane, res);
+        B::open(rh, x);
+        B::open(rr, res);
+        B::open(rg, g);
         float gr = 0.f;
-        if (a.gate && !a.gate_rows) B::load(a.gate, row, a.F, lane, g);
         if (a.gate && a.gate_rows) gr = sigmoid(static_cast<float>(static_cast<const T *>(a.gate)[row]));
+        if (row + step < a.N) fetch(row + step);  // on its way while this row is worked on
         if (a.post) {
             B::normalise(x, a, lane, lds);
 #pragma unroll
@@ -262,34 +302,65 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void k_block_norm(const Norm a) 
 }
 
 template <typename T, int L, int NV>
-__global__ __launch_bounds__(L < 256 ? 256 : L) void k_block_norm_grad(const Norm a) {
+__global__ __launch_bounds__(threads_of(L)) void k_block_norm_grad(const Norm a) {
     using B = Body<T, L, NV>;
-    constexpr int M = B::M, E = B::E, NT = L < 256 ? 256 : L, R = NT / L;
-    __shared__ float lds[kRowLds];
+    constexpr int M = B::M, E = B::E, NT = threads_of(L), R = NT / L;
+    __shared__ float sums_lds[2 * kRowLds];
+    Sums lds{sums_lds};
     __shared__ float cols[R > 1 ? R * L * M : 1];
     const int lane = threadIdx.x % L;
     float s_sc[M], s_pw[M], s_pb[M], s_w[M], s_b[M];
 #pragma unroll
     for (int k = 0; k < M; ++k) s_sc[k] = s_pw[k] = s_pb[k] = s_w[k] = s_b[k] = 0.f;
-    for (int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L; row < a.N; row += (int64_t)gridDim.x * R) {
+    // parameters and the next row stay in registers where there is room for them (128 a lane in workgroups of 1,024)
+    constexpr bool kRoom = L < 1024, kHold = M <= 8 && kRoom;
+    float h_sc[kHold ? M : 1], h_p[kHold ? M : 1], h_pb[kHold ? M : 1], h_w[kHold ? M : 1];
+    if constexpr (kHold) {
+        B::load_param(a.scale, a.F, lane, 1.f, h_sc);
+        B::load_param(a.post_w, a.F, lane, 1.f, h_p);
+        B::load_param(a.post_b, a.F, lane, 0.f, h_pb);
+        B::load_param(a.w, a.F, lane, 1.f, h_w);
+    }
+    auto param = [&](const float *p, const auto &held, float other, float (&v)[M]) {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int k = 0; k < M; ++k) v[k] = held[k];
+        } else {
+            B::load_param(p, a.F, lane, other, v);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * R;
+    int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+    typename B::Raw rh, rr, rg, ry, rt;
+    auto fetch = [&](int64_t at) {
+        B::fetch(a.h, at, a.F, lane, rh);
+        if (a.residual) B::fetch(a.residual, at, a.F, lane, rr);
+        if (a.gate && !a.gate_rows) B::fetch(a.gate, at, a.F, lane, rg);
+        if (a.grad_y) B::fetch(a.grad_y, at, a.F, lane, ry);
+        if (a.grad_r) B::fetch(a.grad_r, at, a.F, lane, rt);
+    };
+    if (kRoom && row < a.N) fetch(row);
+    for (; row < a.N; row += step) {
+        if (!kRoom) fetch(row);
         float nh[M], sg[M], nr[M], t[M], p[M], gy[M];
-        B::load(a.h, row, a.F, lane, nh);
-        if (a.residual) B::load(a.residual, row, a.F, lane, nr);
-        if (a.gate && !a.gate_rows) B::load(a.gate, row, a.F, lane, sg);
-        if (a.grad_y) B::load(a.grad_y, row, a.F, lane, gy);
-        if (a.grad_r) B::load(a.grad_r, row, a.F, lane, t);
+        B::open(rh, nh);
+        B::open(rr, nr);
+        B::open(rg, sg);
+        B::open(ry, gy);
+        B::open(rt, t);
         float gr = 1.f;
         if (a.gate && a.gate_rows) gr = sigmoid(static_cast<float>(static_cast<const T *>(a.gate)[row]));
+        if (kRoom && row + step < a.N) fetch(row + step);  // on its way while this row is worked on
         float rstd_h = 0.f;
         if (a.post) rstd_h = B::normalise(nh, a, lane, lds);
         float sc[M], u[M];
-        B::load_param(a.scale, a.F, lane, 1.f, sc);
-        B::load_param(a.post_w, a.F, lane, 1.f, p);
+        param(a.scale, h_sc, 1.f, sc);
+        param(a.post_w, h_p, 1.f, p);
 #pragma unroll
         for (int k = 0; k < M; ++k) u[k] = nh[k];
         if (a.post) {
             float pb[M];
-            B::load_param(a.post_b, a.F, lane, 0.f, pb);
+            param(a.post_b, h_pb, 0.f, pb);
 #pragma unroll
             for (int k = 0; k < M; ++k) u[k] = fmaf(nh[k], p[k], pb[k]);
         }
@@ -303,7 +374,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void k_block_norm_grad(const Nor
         if (a.pre && a.grad_y) {
             const float rstd_r = B::normalise(nr, a, lane, lds);
             float w[M];
-            B::load_param(a.w, a.F, lane, 1.f, w);
+            param(a.w, h_w, 1.f, w);
 #pragma unroll
             for (int k = 0; k < M; ++k) {
                 s_w[k] = fmaf(gy[k], nr[k], s_w[k]);
@@ -395,47 +466,67 @@ __global__ __launch_bounds__(1024) void k_join_columns(const float *__restrict__
     }
 }
 
-int64_t most_groups(int64_t N, int F) { return F <= 512 ? 1024 : 512; }
+// Workgroups of the backward: 4,096 wavefronts (2,048 of rows of two), so that the sums they leave are few.
+int64_t most_groups(int L) { return L == 128 ? 1024 : 4096 * 64 / threads_of(L); }
 
 struct Shape {
     int L, NV;
 };
-// Lanes of a row: groups of 16 up to one piece each, a wavefront up to two, then workgroups.
-Shape shape_of(int64_t F, int E) {
+// Lanes of a row and pieces a lane. The backward holds five arrays of a row and as many sums, so a lane has at most 8
+// values there where a wider workgroup can take the rest: 16,000 rows of 1,433 (fp32) 185 us with 512
+// lanes of one piece, 210 with 256 of two; the forward 111 and 82.
+Shape shape_of(int64_t F, int E, bool backward) {
     const int64_t v = (F + E - 1) / E;
-    if (v <= 16) return {16, 1};
-    if (v <= 64) return {64, 1};
-    if (v <= 128) return {64, 2};
+    const bool two = !backward || E == 4;  // two pieces of 4 values in the backward
+    for (int L = 8; L <= 64; L *= 2)
+        if (v <= L) return {L, 1};
+    if (v <= 128) return two ? Shape{64, 2} : Shape{128, 1};
     if (v <= 256) return {256, 1};
-    if (v <= 512) return {256, 2};
-    if (v <= 1024) return {512, 2};
+    if (v <= 512) return backward ? Shape{512, 1} : Shape{256, 2};
+    if (v <= 1024) return two ? Shape{512, 2} : Shape{1024, 1};
     return {1024, 2};
 }
 
-template <typename T, int L, int NV>
-int launch(const Norm &a, bool backward, int64_t groups, hipStream_t s) {
-    constexpr int NT = L < 256 ? 256 : L, R = NT / L;
-    if (backward) k_block_norm_grad<T, L, NV><<<static_cast<unsigned>(groups), NT, 0, s>>>(a);
+template <typename T, int L, int NV, bool BACKWARD>
+int launch(const Norm &a, int64_t groups, hipStream_t s) {
+    constexpr int NT = threads_of(L), R = NT / L;
+    if constexpr (BACKWARD) k_block_norm_grad<T, L, NV><<<static_cast<unsigned>(groups), NT, 0, s>>>(a);
     else k_block_norm<T, L, NV><<<grid_for(a.N, R, 2048 * 256 / NT), NT, 0, s>>>(a);
     PYG_LAUNCH_CHECK();
     return PYG_OK;
 }
 
-template <typename T>
-int by_shape(const Norm &a, bool backward, int64_t groups, hipStream_t s) {
-    const Shape h = shape_of(a.F, 16 / sizeof(T));
-    if (h.L == 16) return launch<T, 16, 1>(a, backward, groups, s);
-    if (h.L == 64) return h.NV == 1 ? launch<T, 64, 1>(a, backward, groups, s) : launch<T, 64, 2>(a, backward, groups, s);
-    if (h.L == 256) return h.NV == 1 ? launch<T, 256, 1>(a, backward, groups, s) : launch<T, 256, 2>(a, backward, groups, s);
-    if constexpr (sizeof(T) == 4)
-        if (h.L == 1024) return launch<T, 1024, 2>(a, backward, groups, s);  // bf16 rows end at 1,024 pieces
-    return launch<T, 512, 2>(a, backward, groups, s);
+template <typename T, bool BACKWARD>
+int by_shape(const Norm &a, int64_t groups, hipStream_t s) {
+    constexpr int E = 16 / sizeof(T);
+    constexpr bool two = !BACKWARD || E == 4;
+    const Shape h = shape_of(a.F, E, BACKWARD);
+    if (h.L == 8) return launch<T, 8, 1, BACKWARD>(a, groups, s);
+    if (h.L == 16) return launch<T, 16, 1, BACKWARD>(a, groups, s);
+    if (h.L == 32) return launch<T, 32, 1, BACKWARD>(a, groups, s);
+    if (h.L == 64 && h.NV == 1) return launch<T, 64, 1, BACKWARD>(a, groups, s);
+    if (h.L == 256 && h.NV == 1) return launch<T, 256, 1, BACKWARD>(a, groups, s);
+    if constexpr (two) {
+        if (h.L == 64) return launch<T, 64, 2, BACKWARD>(a, groups, s);
+        if (h.L == 512 && h.NV == 2) return launch<T, 512, 2, BACKWARD>(a, groups, s);
+    } else {
+        if (h.L == 128) return launch<T, 128, 1, BACKWARD>(a, groups, s);
+        if (h.L == 1024) return launch<T, 1024, 1, BACKWARD>(a, groups, s);
+    }
+    if constexpr (BACKWARD) {
+        if (h.L == 512) return launch<T, 512, 1, BACKWARD>(a, groups, s);
+    } else {
+        if (h.L == 256) return launch<T, 256, 2, BACKWARD>(a, groups, s);
+    }
+    if constexpr (E == 4)
+        if (h.L == 1024) return launch<T, 1024, 2, BACKWARD>(a, groups, s);
+    return PYG_ERR_UNSUPPORTED;  // not reached: F <= 8192
 }
 
 int64_t grad_groups(const pyg_block_norm_args *c) {
     const int E = c->dtype == PYG_BF16 ? 8 : 4;
-    const Shape h = shape_of(c->F, E);
-    const int64_t R = (h.L < 256 ? 256 : h.L) / h.L, rows = (c->N + R - 1) / R, most = most_groups(c->N, (int)c->F);
+    const Shape h = shape_of(c->F, E, true);
+    const int64_t R = threads_of(h.L) / h.L, rows = (c->N + R - 1) / R, most = most_groups(h.L);
     return rows < 1 ? 1 : rows < most ? rows : most;
 }
 
@@ -473,7 +564,7 @@ extern "C" int pyg_block_norm(const pyg_block_norm_args *c, void *r, void *y, in
     Norm a = fill(c);
     a.r = r, a.y = y, a.codes = codes, a.steps = steps;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return c->dtype == PYG_BF16 ? by_shape<__bf16>(a, false, 0, s) : by_shape<float>(a, false, 0, s);
+    return c->dtype == PYG_BF16 ? by_shape<__bf16, false>(a, 0, s) : by_shape<float, false>(a, 0, s);
 }
 
 extern "C" int pyg_block_norm_backward_workspace(const pyg_block_norm_args *c, size_t *bytes) {
@@ -510,7 +601,8 @@ extern "C" int pyg_block_norm_backward(const pyg_block_norm_args *c, const void 
     a.need_w = place(grad_weight), a.need_b = place(grad_bias);
     a.sums = n;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    PYG_TRY(c->dtype == PYG_BF16 ? by_shape<__bf16>(a, true, groups, s) : by_shape<float>(a, true, groups, s));
+    const int rc = c->dtype == PYG_BF16 ? by_shape<__bf16, true>(a, groups, s) : by_shape<float, true>(a, groups, s);
+    if (rc != PYG_OK) return rc;
     if (n > 0) {
         const int64_t all = (int64_t)n * a.F;
         k_join_columns<<<static_cast<unsigned>((all + 63) / 64), 1024, 0, s>>>(a.part, static_cast<int>(groups), n, a.F, cols);

@@ -529,7 +529,10 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
 
 template <typename T, int DP>
 int by_waves(const BackwardArgs &b, void *ws, hipStream_t s) {
-    if (b.f.Nq <= 64 * b.f.B) return launch<T, DP, 1, 32>(b, ws, s);
+    // lone wavefronts for small graphs, as in the forward, and where tiles of 128 are few: one graph of 1,024 nodes
+    // (4 heads of 64, bf16) 111 us against 126, 16 of 512 83 against 100; one of 4,096 (8 heads) 315 against 281.
+    const int64_t n = b.f.Nq, g = b.f.B;
+    if (n <= 128 * g || (n <= 1024 * g && n / 128 * b.f.H <= 256)) return launch<T, DP, 1, 32>(b, ws, s);
     return launch<T, DP, 4, DP * sizeof(T) <= 128 ? 64 : 32>(b, ws, s);
 }
 

@@ -120,6 +120,9 @@ CASES = [  # rows, features, norm, gate, parts
     (3, 8192, "layer", "full", ALL),
     (40, 1, "rms", "full", ALL),
     (11, 96, "layer", "full", ("residual", "post_weight")),
+    (700, 900, "layer", "full", ALL),
+    (600, 1600, "rms", "row", ALL),
+    (530, 3000, "layer", "full", ("residual", "scale", "weight", "bias")),
 ]
 
 
