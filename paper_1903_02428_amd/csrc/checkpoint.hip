@@ -87,6 +87,30 @@ constexpr int kTileI = 128, kTileO = 128, kTileN = 32;
 typedef __bf16 bf16;
 using Rows = attn::Tile<bf16, 128>;
 
+// One 16-byte piece of an operand as PARTS bf16 pieces, part k at place(k): bf16 values as they are, fp32 ones
+// cut into their first, second and last 8 significant bits.
+template <typename T, int PARTS, typename PLACE>
+__device__ __forceinline__ void put_parts(uint4 piece, PLACE place) {
+    if constexpr (PARTS == 1) {
+        *reinterpret_cast<uint4 *>(place(0)) = piece;
+    } else {
+        attn::Piece<T> v;
+        v.u = piece;
+        float f[4] = {v.v[0], v.v[1], v.v[2], v.v[3]};
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+            uint32_t b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                b[e] = __float_as_uint(f[e]) & 0xFFFF0000u;
+                // an infinity or NaN is all in the first part
+                f[e] = (b[e] & 0x7F800000u) == 0x7F800000u ? 0.f : f[e] - __uint_as_float(b[e]);
+            }
+            *reinterpret_cast<uint2 *>(place(k)) = make_uint2(b[0] >> 16 | b[1], b[2] >> 16 | b[3]);
+        }
+    }
+}
+
 // A workgroup owns 128 x 128 of dTheta and every splits-th tile of 32 rows. PARTS
 // bf16 parts of G (1: bf16 G, 3: fp32 G).
 template <typename T, int PARTS>
@@ -144,25 +168,9 @@ __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
             const int p = j * kBlock + threadIdx.x, r = p / (kTileO / E), c = p % (kTileO / E) * E;
-            if constexpr (PARTS == 1) {
-                *reinterpret_cast<uint4 *>(gt[0] + r * Rows::kRowBytes + ((c / 8 ^ attn::swizzle<Rows::C>(r)) << 4)) = cg[j];
-            } else {
-                attn::Piece<T> v;
-                v.u = cg[j];
-                float f[4] = {v.v[0], v.v[1], v.v[2], v.v[3]};
-#pragma unroll
-                for (int k = 0; k < PARTS; ++k) {
-                    uint32_t b[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        b[e] = __float_as_uint(f[e]) & 0xFFFF0000u;
-                        // an infinity or NaN is all in the first part
-                        f[e] = (b[e] & 0x7F800000u) == 0x7F800000u ? 0.f : f[e] - __uint_as_float(b[e]);
-                    }
-                    *reinterpret_cast<uint2 *>(gt[k] + r * Rows::kRowBytes + ((c / 8 ^ attn::swizzle<Rows::C>(r)) << 4) + c % 8 * 2) =
-                        make_uint2(b[0] >> 16 | b[1], b[2] >> 16 | b[3]);
-                }
-            }
+            put_parts<T, PARTS>(cg[j], [&](int k) {
+                return gt[k] + r * Rows::kRowBytes + ((c / 8 ^ attn::swizzle<Rows::C>(r)) << 4) + c % 8 * 2;
+            });
         }
     };
     int64_t n0 = (int64_t)sp * kTileN;
@@ -203,6 +211,98 @@ __global__ __launch_bounds__(kBlock) void k_theta_grad(const uint8_t *__restrict
         }
 }
 
+// ------------------------------------------------------------- dX = G Theta^T
+
+// Both operands contract over the features o they hold adjacent, so rows go to LDS as they lie
+// and come back as row pieces. fp32 operands are three bf16 parts each; of the nine products the six are taken
+// that reach the first 24 bits (parts a, b with a + b <= 2), smallest first: 2.6 times the rate
+// that fp32 instructions have. A workgroup owns 128 rows and 128 of the Fi columns, a wavefront
+// 64 x 64; Theta is the A operand, so that a lane ends with four adjacent features of one row.
+template <typename T, int PARTS>
+__global__ __launch_bounds__(kBlock) void k_input_grad(const T *__restrict__ g, const T *__restrict__ theta, int64_t N, int Fi,
+                                                       int Fo, int tiles_i, bool vec, T *__restrict__ out) {
+    using Rows = attn::Tile<bf16, 32>;
+    constexpr int E = 16 / sizeof(T), GP = 128 * 32 / E / kBlock;
+    __shared__ __align__(16) char gt[PARTS][Rows::bytes<128>()], tt[PARTS][Rows::bytes<128>()];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int64_t n0 = (int64_t)(blockIdx.x / tiles_i) * 128;
+    const int i0 = blockIdx.x % tiles_i * 128;
+    const int wi = wave / 2 * 2, wn = wave % 2 * 2;  // the wavefront's blocks of 32
+    const Rows::RowLane rl(lane);
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[a][b] = f32x16(0.f);
+    uint4 cg[GP], ct[GP];
+    auto load = [&](int o0) {
+#pragma unroll
+        for (int j = 0; j < GP; ++j) {
+            const int p = j * kBlock + threadIdx.x, r = p / (32 / E), c = o0 + p % (32 / E) * E;
+            cg[j] = attn::load_piece<T>(g + (n0 + r) * Fo, c, Fo, n0 + r < N);
+            ct[j] = attn::load_piece<T>(theta + (int64_t)(i0 + r) * Fo, c, Fo, i0 + r < Fi);
+        }
+    };
+    auto store = [&](const uint4 (&v)[GP], char (&tile)[PARTS][Rows::bytes<128>()]) {
+#pragma unroll
+        for (int j = 0; j < GP; ++j) {
+            const int p = j * kBlock + threadIdx.x, r = p / (32 / E), c = p % (32 / E) * E;
+            put_parts<T, PARTS>(v[j], [&](int k) {
+                return tile[k] + r * Rows::kRowBytes + ((c / 8 ^ attn::swizzle<Rows::C>(r)) << 4) + c % 8 * 2;
+            });
+        }
+    };
+    load(0);
+    for (int o0 = 0; o0 < Fo; o0 += 32) {
+        __syncthreads();
+        store(cg, gt);
+        store(ct, tt);
+        __syncthreads();
+        if (o0 + 32 < Fo) load(o0 + 32);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            uint4 a[PARTS][2], b[PARTS][2];
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    a[k][t] = Rows::row_piece(tt[k], rl, wi + t, u);
+                    b[k][t] = Rows::row_piece(gt[k], rl, wn + t, u);
+                }
+#pragma unroll
+            for (int sum = PARTS - 1; sum >= 0; --sum)
+#pragma unroll
+                for (int k = 0; k <= sum; ++k)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) acc[x][y] = attn::mma<bf16>(a[k][x], b[sum - k][y], acc[x][y]);
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        const int64_t n = n0 + 32 * (wn + y) + (lane & 31);
+        if (n >= N) continue;
+        T *o = out + n * Fi;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int i = i0 + 32 * (wi + x) + 8 * q + 4 * h;
+                if (i >= Fi) continue;
+                const float v[4] = {acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+                if (vec) {
+                    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(o + i) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *reinterpret_cast<uint2 *>(o + i) = make_uint2(attn::pack_bf16(v[0], v[1]), attn::pack_bf16(v[2], v[3]));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < Fi) o[i + e] = T(v[e]);
+                }
+            }
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_join_theta(const float *__restrict__ part, int64_t n, int splits,
                                                        T *__restrict__ out) {
@@ -222,19 +322,13 @@ __global__ __launch_bounds__(kBlock) void k_join_theta(const float *__restrict__
     }
 }
 
-// Theta [Fi, Fo] -> Theta^T [Fo, Fi].
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_transpose(const T *__restrict__ in, int64_t Fi, int64_t Fo, T *__restrict__ out) {
-    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < Fi * Fo; i += (int64_t)gridDim.x * kBlock)
-        out[i] = in[i % Fi * Fo + i / Fi];
-}
-
 constexpr int64_t kMax32 = int64_t(1) << 31, kMaxF = int64_t(1) << 24;
 
-// Row ranges of dTheta: two workgroups a CU, 256 rows or more each.
+// Row ranges of dTheta: two workgroups a CU, 128 rows or more each (19,717 rows, 500 to 64 features, bf16:
+// 256 rows 20 us, 128 18).
 int splits_of(int64_t N, int64_t Fi, int64_t Fo) {
     const int64_t tiles = ((Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO);
-    int64_t s = 512 / tiles, most = N / 256;
+    int64_t s = 512 / tiles, most = N / 128;
     s = s < most ? s : most;
     return static_cast<int>(s < 1 ? 1 : s);
 }
@@ -298,57 +392,52 @@ extern "C" int pyg_checkpoint_restore(const int8_t *codes, const uint8_t *steps,
 
 namespace {
 
-struct Layout {
-    size_t bytes;
-    void *theta_t, *dense;
-    size_t dense_bytes;
-    float *part;
-};
-int layout(int dtype, int64_t N, int64_t Fi, int64_t Fo, void *ws, Layout *l) {
+int check_dense(int dtype, int64_t N, int64_t Fi, int64_t Fo, size_t *bytes) {
     if ((dtype != PYG_F32 && dtype != PYG_BF16) || N < 0 || Fi < 1 || Fo < 1) return PYG_ERR_INVALID_ARG;
     if (N >= kMax32 || Fi >= kMaxF || Fo >= kMaxF) return PYG_ERR_UNSUPPORTED;
-    PYG_TRY(pyg_dense_transform_workspace(Fo, Fi, &l->dense_bytes));
-    Carver c(ws);
-    l->part = c.take<float>(static_cast<size_t>(splits_of(N, Fi, Fo)) * Fi * Fo);
-    l->theta_t = c.take<char>(static_cast<size_t>(Fi) * Fo * (dtype == PYG_BF16 ? 2 : 4));
-    l->dense = c.take<char>(l->dense_bytes);
-    l->bytes = align_up(c.used, 256);
+    *bytes = static_cast<size_t>(splits_of(N, Fi, Fo)) * Fi * Fo * sizeof(float);
+    return PYG_OK;
+}
+
+template <typename T>
+int input_grad(const T *g, const T *theta, int64_t N, int Fi, int Fo, T *out, hipStream_t s) {
+    const int tiles_i = (Fi + 127) / 128;
+    const int64_t grid = (N + 127) / 128 * tiles_i;
+    if (grid * kBlock >= (int64_t(1) << 32)) return PYG_ERR_UNSUPPORTED;
+    k_input_grad<T, sizeof(T) == 2 ? 1 : 3><<<static_cast<unsigned>(grid), kBlock, 0, s>>>(
+        g, theta, N, Fi, Fo, tiles_i, Fi % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0, out);
+    PYG_LAUNCH_CHECK();
     return PYG_OK;
 }
 
 }  // namespace
 
 extern "C" int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int64_t Fo, size_t *bytes) {
-    Layout l{};
-    if (!bytes) return PYG_ERR_INVALID_ARG;
-    PYG_TRY(layout(dtype, N, Fi, Fo, nullptr, &l));
-    *bytes = l.bytes;
-    return PYG_OK;
+    return bytes ? check_dense(dtype, N, Fi, Fo, bytes) : PYG_ERR_INVALID_ARG;
 }
 
 extern "C" int pyg_dense_transform_backward(const void *grad_out, int dtype, int64_t N, int64_t Fo, const void *theta,
                                             int64_t Fi, const int8_t *codes, const uint8_t *steps, void *grad_x,
                                             void *grad_theta, void *ws, size_t ws_bytes, void *stream) {
-    Layout l{};
-    PYG_TRY(layout(dtype, N, Fi, Fo, ws, &l));
+    size_t need = 0;
+    PYG_TRY(check_dense(dtype, N, Fi, Fo, &need));
     if (N > 0 && !grad_out) return PYG_ERR_INVALID_ARG;
-    if (grad_x && !theta) return PYG_ERR_INVALID_ARG;
+    if (grad_x && N > 0 && !theta) return PYG_ERR_INVALID_ARG;
     if (grad_theta && N > 0 && (!codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16)) return PYG_ERR_INVALID_ARG;
-    if (ws_bytes < l.bytes || !ws) return PYG_ERR_WORKSPACE;
+    if (ws_bytes < need || !ws) return PYG_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (grad_x && N > 0) {
-        const unsigned grid = grid_for(Fi * Fo, kBlock, 4096);
-        if (dtype == PYG_BF16)
-            k_transpose<uint16_t><<<grid, kBlock, 0, s>>>(static_cast<const uint16_t *>(theta), Fi, Fo, static_cast<uint16_t *>(l.theta_t));
-        else
-            k_transpose<uint32_t><<<grid, kBlock, 0, s>>>(static_cast<const uint32_t *>(theta), Fi, Fo, static_cast<uint32_t *>(l.theta_t));
-        PYG_LAUNCH_CHECK();
-        PYG_TRY(pyg_dense_transform(grad_out, dtype, N, Fo, l.theta_t, Fi, grad_x, dtype, l.dense, l.dense_bytes, stream));
-    }
-    if (!grad_theta) return PYG_OK;
     const int fi = static_cast<int>(Fi), fo = static_cast<int>(Fo);
+    float *part = static_cast<float *>(ws);
+    int rc = PYG_OK;
+    if (grad_x && N > 0) {
+        rc = dtype == PYG_BF16 ? input_grad(static_cast<const __bf16 *>(grad_out), static_cast<const __bf16 *>(theta), N, fi, fo,
+                                            static_cast<__bf16 *>(grad_x), s)
+                               : input_grad(static_cast<const float *>(grad_out), static_cast<const float *>(theta), N, fi, fo,
+                                            static_cast<float *>(grad_x), s);
+    }
+    if (rc != PYG_OK || !grad_theta) return rc;
     return dtype == PYG_BF16 ? theta_grad(static_cast<const __bf16 *>(grad_out), N, fo, fi, codes, steps,
-                                          static_cast<__bf16 *>(grad_theta), l.part, s)
+                                          static_cast<__bf16 *>(grad_theta), part, s)
                              : theta_grad(static_cast<const float *>(grad_out), N, fo, fi, codes, steps,
-                                          static_cast<float *>(grad_theta), l.part, s);
+                                          static_cast<float *>(grad_theta), part, s);
 }

@@ -299,22 +299,26 @@ def checkpoint_restore(kept: Checkpoint, dtype: torch.dtype | None = None, out: 
     return out
 
 
-def dense_transform_backward(grad_out: torch.Tensor, theta: torch.Tensor, kept: Checkpoint, need_grad_x: bool = True,
+def dense_transform_backward(grad_out: torch.Tensor, theta: torch.Tensor, kept: Checkpoint | None, need_grad_x: bool = True,
                              need_grad_theta: bool = True, workspace: torch.Tensor | None = None):
     """Gradients of dense_transform(x, theta) from grad_out [N, Fo] and x kept in 8 bits:
-    (grad_x = grad_out theta^T or None, grad_theta = x^T grad_out or None), in theta's type."""
+    (grad_x = grad_out theta^T or None, grad_theta = x^T grad_out or None), in theta's type. Without
+    need_grad_theta nothing of x is read, and kept may be None."""
     lib = library()
     _need_cuda("grad_out", grad_out, None, 2)
     if grad_out.dtype not in DTYPE:
         raise ValueError("grad_out must be float32 or bfloat16")
     _need_cuda("theta", theta, grad_out.dtype, 2)
     dev = grad_out.device
-    _checked(kept, dev)
+    if kept is not None:
+        _checked(kept, dev)
+    elif need_grad_theta:
+        raise ValueError("the gradient of theta needs x's checkpoint")
     (N, Fo), Fi = grad_out.shape, theta.shape[0]
-    if theta.shape[1] != Fo or kept.N != N or kept.F != Fi:
+    if theta.shape[1] != Fo or (kept is not None and (kept.N, kept.F) != (N, Fi)):
         raise ValueError("grad_out must be [N, Fo], theta [Fi, Fo] and the checkpoint [N, Fi]")
-    if Fo < 1:
-        raise ValueError("theta must have columns")
+    if Fo < 1 or Fi < 1:
+        raise ValueError("theta must have rows and columns")
     _same_device(dev, theta=theta, workspace=workspace)
     gx = torch.empty((N, Fi), dtype=theta.dtype, device=dev) if need_grad_x else None
     gt = torch.empty_like(theta) if need_grad_theta else None
@@ -323,7 +327,7 @@ def dense_transform_backward(grad_out: torch.Tensor, theta: torch.Tensor, kept: 
         if workspace is None or workspace.numel() < nbytes:
             workspace = _workspace(nbytes, dev)
         _check(lib.pyg_dense_transform_backward(_ptr(grad_out), DTYPE[theta.dtype], N, Fo, _ptr(theta), Fi,
-                                                _ptr(kept.codes), _ptr(kept.steps), _ptr(gx), _ptr(gt), _ptr(workspace),
+                                                _ptr(kept.codes) if kept else None, _ptr(kept.steps) if kept else None, _ptr(gx), _ptr(gt), _ptr(workspace),
                                                 workspace.numel(), _stream(dev)), "pyg_dense_transform_backward")
     return gx, gt
 
@@ -352,10 +356,9 @@ class DenseTransform(torch.autograd.Function):
     def backward(ctx, grad_out):
         theta, *held = ctx.saved_tensors
         g, t = grad_out.to(theta.dtype).contiguous(), theta.detach().contiguous()
+        # where theta needs no gradient nothing was kept
         kept = Checkpoint(*held, ctx.F, theta.dtype) if ctx.F else None
-        if kept is None:  # the weights need no gradient: nothing was kept
-            return (dense_transform(g, t.t().contiguous(), theta.dtype), None, None)
-        gx, gt = dense_transform_backward(g, t, kept, ctx.needs_input_grad[0], True)
+        gx, gt = dense_transform_backward(g, t, kept, ctx.needs_input_grad[0], kept is not None)
         return gx, gt, None
 
 
