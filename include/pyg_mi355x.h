@@ -759,8 +759,10 @@ int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
  * gives zeros, and zero gradients. Scores, sums and statistics are fp32; bf16
  * weights p are rounded to bf16 for the second product. Deterministic.
  * Errors: PYG_ERR_INVALID_ARG (NULL or negative or inconsistent arguments,
- * Hkv not dividing H, scale not in (0, 1e30], overlapping strides),
- * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 1024, rows >= 2^31, a grid
+ * Hkv not dividing H, scale not in [1e-30, 1e30], overlapping strides, results that overlap
+ * the inputs),
+ * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 1024, rows >= 2^31, row
+ * strides >= 2^22 elements, a grid
  * beyond 2^32 threads), PYG_ERR_WORKSPACE. */
 int pyg_global_attention(const pyg_attention *a, const void *q, const void *k, const void *v, void *out, float *stat,
                          void *rest, void *ws, size_t ws_bytes, void *stream);
@@ -798,7 +800,7 @@ typedef struct {
 
 /* r and y [N, F] in dtype, each rounded once (y is taken of the unrounded r; r may be NULL
  * where y is made). codes and steps, or NULL: y as it was stored, in 8 bits (see
- * pyg_activation_checkpoint). Statistics are fp32, two-pass. Deterministic.
+ * pyg_activation_checkpoint). Statistics are fp32, two-pass. Results may not overlap the inputs. Deterministic.
  * Errors: PYG_ERR_INVALID_ARG (bad dtype or norm, missing arrays, y without weight or
  * weight without y, codes without y, eps < 0), PYG_ERR_UNSUPPORTED (F > 8192, N >= 2^31). */
 int pyg_block_norm(const pyg_block_norm_args *a, void *r, void *y, int8_t *codes, uint8_t *steps, void *stream);

@@ -204,9 +204,13 @@ using namespace attn;
 
 constexpr int64_t kMax32 = int64_t(1) << 31;
 
-// Query rows that share a key head, on average over the graphs, up to which
-// the 16-row form takes them.
-bool few(const Args &a) { return a.Nq * a.G <= 16 * a.B; }
+// Whether the 16-row form takes the queries: up to 16 rows that share a key head, on average over the graphs; or more,
+// where whole walks over long histories would be too few for the card (bf16: one query of 32 heads on
+// one over 100,000 keys 62 us instead of 3,726, 64 queries of 8 heads over as many 145 instead of 3,236).
+bool few(const Args &a) {
+    if (a.Nq * a.G <= 16 * a.B) return true;
+    return (a.Nq / 32 + a.B) * a.H < 512 && a.Nk >= 1024 * a.B && a.Nq * 16 <= a.Nk;
+}
 
 bool vectors(const void *p, int64_t row, int64_t head, int64_t D, size_t e) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && row * e % 16 == 0 && head * e % 16 == 0 && D * e % 16 == 0;
@@ -217,7 +221,7 @@ int take(const pyg_attention *c, Args *a) {
     if (!c) return PYG_ERR_INVALID_ARG;
     if (c->dtype != PYG_F32 && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
     if (c->B < 0 || c->Nq < 0 || c->Nk < 0 || c->H < 1 || c->Hkv < 1 || c->D < 1 || c->H % c->Hkv) return PYG_ERR_INVALID_ARG;
-    if (!(c->scale > 0.f) || c->scale > 1e30f) return PYG_ERR_INVALID_ARG;
+    if (!(c->scale >= 1e-30f) || c->scale > 1e30f) return PYG_ERR_INVALID_ARG;
     if (c->Nq >= kMax32 || c->Nk >= kMax32 || c->B >= kMax32 || c->D > 128 || c->H > 65535) return PYG_ERR_UNSUPPORTED;
     if (c->table) {
         if (!c->bucket || c->buckets < 1 || c->reach < 0) return PYG_ERR_INVALID_ARG;
@@ -261,6 +265,19 @@ int take_inputs(const pyg_attention *c, const void *q, const void *k, const void
     return PYG_OK;
 }
 
+// Whether n elements at p meet the N rows of H heads at x.
+bool meets(const void *p, int64_t n, const void *x, int64_t N, int64_t H, int64_t D, int64_t row, int64_t head, size_t e) {
+    if (!p || !x || n <= 0 || N <= 0) return false;
+    const uintptr_t p0 = reinterpret_cast<uintptr_t>(p), x0 = reinterpret_cast<uintptr_t>(x);
+    const uintptr_t span = static_cast<uintptr_t>(row * (N - 1) + head * (H - 1) + D) * e;
+    return p0 < x0 + span && x0 < p0 + static_cast<uintptr_t>(n) * e;
+}
+bool meets_inputs(const pyg_attention *c, const Args &a, const void *p, int64_t n) {
+    const size_t e = bytes_of(c);
+    return meets(p, n, a.q, a.Nq, a.H, a.D, a.q_row, a.q_head, e) || meets(p, n, a.k, a.Nk, a.Hkv, a.D, a.k_row, a.k_head, e) ||
+           meets(p, n, a.v, a.Nk, a.Hkv, a.D, a.v_row, a.v_head, e);
+}
+
 }  // namespace
 }  // namespace pyg
 
@@ -288,6 +305,7 @@ extern "C" int pyg_global_attention(const pyg_attention *c, const void *q, const
     PYG_TRY(pyg_global_attention_workspace(c, &need));
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     if (a.Nq == 0) return PYG_OK;
+    if (meets_inputs(c, a, out, a.Nq * a.H * a.D) || meets_inputs(c, a, rest, a.Nq * a.H * a.D)) return PYG_ERR_INVALID_ARG;
     if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
     a.out = out, a.stat = stat, a.rest = rest;
     a.vec_o = vectors(out, a.D, a.D, a.D, bytes_of(c)) && vectors(rest, a.D, a.D, a.D, bytes_of(c));
@@ -314,6 +332,9 @@ extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void 
     if (a.Nq > 0 && (!grad_out || !out || !stat || !grad_q)) return PYG_ERR_INVALID_ARG;
     if (a.Nk > 0 && (!grad_k || !grad_v)) return PYG_ERR_INVALID_ARG;
     if (grad_table && !c->table) return PYG_ERR_INVALID_ARG;
+    if (meets_inputs(c, a, grad_q, a.Nq * a.H * a.D) || meets_inputs(c, a, grad_k, a.Nk * a.Hkv * a.D) ||
+        meets_inputs(c, a, grad_v, a.Nk * a.Hkv * a.D))
+        return PYG_ERR_INVALID_ARG;
     const size_t need = attn::backward_workspace(a);
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;

@@ -69,7 +69,7 @@ constexpr bool kValuesInLds = DP == 128 && sizeof(T) == 2;
 // A workgroup owns 32 * WAVES queries, as in the forward.
 template <typename T, int DP, int WAVES, int BK>
 __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(const BackwardArgs b, int64_t nslots, float *__restrict__ delta,
-                                                       float *__restrict__ part) {
+                                                       float *__restrict__ part, int splits, float *__restrict__ dq_part) {
     const Args &a = b.f;
     constexpr int NT = 64 * WAVES, BM = 32 * WAVES, E = Elem<T>::E, SQ = DP / (2 * E), NK = BK / 32;
     using L = Tile<T, DP>;
@@ -81,15 +81,20 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     const int lane = threadIdx.x & 63, wave = to_scalar(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
     const uint32_t id = blockIdx.x;
     const int hk = id % a.Hkv, head = hk * a.G + id / a.Hkv % a.G;
-    const int64_t slot = nslots - 1 - id / a.H;
-    float *mine = part ? part + (slot * a.H + head) * a.buckets : nullptr;  // the workgroup's share of dT
+    const int sp = id / a.H % splits;  // the workgroup's share of the keys
+    const int64_t slot = nslots - 1 - id / a.H / splits;
+    float *mine = part ? part + ((slot * splits + sp) * a.H + head) * a.buckets : nullptr;  // its share of dT
+    dq_part += sp * a.Nq * a.H * a.D;
     const Place pq = place_of(a.q_ptr, a.B, a.Nq, slot, BM, 1, lane);
     const int64_t q0 = pq.first + pq.tile * BM;
     if (pq.tile < 0 || q0 >= pq.last || pq.graph == a.B) {
         if (mine)
             for (int i = threadIdx.x; i < a.buckets; i += NT) mine[i] = 0.f;
-        if (pq.graph == a.B && pq.tile >= 0 && q0 < pq.last)
-            zero_rows(static_cast<T *>(b.grad_q), q0, q0 + BM < pq.last ? q0 + BM : pq.last, a.H, head, a.D);
+        if (pq.graph == a.B && pq.tile >= 0 && q0 < pq.last) {
+            const int64_t e = q0 + BM < pq.last ? q0 + BM : pq.last;
+            if (splits > 1) zero_rows(dq_part, q0, e, a.H, head, a.D);
+            else zero_rows(static_cast<T *>(b.grad_q), q0, e, a.H, head, a.D);
+        }
         return;
     }
     const int offsets = 2 * a.reach + 1;
@@ -111,6 +116,12 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         const int64_t seen = pq.tile * BM + BM + nk - nq;
         end = seen < nk ? (seen < 0 ? 0 : seen) : nk;
     }
+    int64_t from = 0;
+    if (splits > 1) {
+        const int64_t share = ((nk + BK - 1) / BK + splits - 1) / splits * BK;
+        from = sp * share;
+        end = end < from + share ? end : from + share;
+    }
     const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
     auto fetch = [&](int64_t j0, int half) {
         if (j0 >= end) return;
@@ -118,7 +129,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         sv.load(vb, j0, nk - j0, lds + (2 * half + 1) * kTile);
     };
     // the first tile, the bias and the queries' rows wait for memory together
-    fetch(0, 0);
+    fetch(from, 0);
     const bool wild = stage_bias<T>(a, head, bias, mine ? bucket : nullptr);
     const int64_t safe = there ? row : pq.first, at = (safe * a.H + head) * a.D;
     float dl = 0.f;
@@ -142,7 +153,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     float2 raw = make_float2(kNegInf, 0.f);
     if (there) {
         raw = *reinterpret_cast<const float2 *>(a.stat + (row * a.H + head) * 2);
-        if (h == 0) delta[row * a.H + head] = dl;
+        if (h == 0 && sp == 0) delta[row * a.H + head] = dl;
     }
     const RowStat st = row_stat(raw, a.c2);
     constexpr bool kDeltaFirst = DP < 128 && !kStartLate<T>;  // dP starts from it, but where registers are short
@@ -222,8 +233,8 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
             }
     };
     if constexpr (HALVES == 1) {
-        for (int64_t j0 = 0; j0 < end; j0 += BK) {
-            if (j0 > 0) {
+        for (int64_t j0 = from; j0 < end; j0 += BK) {
+            if (j0 > from) {
                 __syncthreads();
                 fetch(j0, 0);
             }
@@ -232,7 +243,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
             step(lds, lds + kTile, j0);
         }
     } else {
-        for (int64_t j0 = 0; j0 < end; j0 += 2 * BK) {
+        for (int64_t j0 = from; j0 < end; j0 += 2 * BK) {
             loads_done();
             __syncthreads();
             fetch(j0 + BK, 1);
@@ -244,7 +255,8 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
             step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
         }
     }
-    store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
+    if (splits > 1) store_rows<float, DP>(dq_part, row, there, a.H, head, a.D, a.D % 4 == 0, acc, a.scale, lane);
+    else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
     if (mine) {
         below = wave_sum(below), above = wave_sum(above);
         if (lane == 0) own[0] += below, own[offsets - 1] += above;
@@ -469,6 +481,24 @@ int kv_splits(const Args &a, int64_t tiles) {
     }
     return s;
 }
+// dQ from the shares of the key ranges [splits][Nq, H, D], in order.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_join_q(const float *__restrict__ part, int64_t n, int splits, T *__restrict__ dq) {
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+        float x = 0.f;
+        for (int s = 0; s < splits; ++s) x += part[s * n + i];
+        dq[i] = T(x);
+    }
+}
+// Key ranges of dQ, where few queries over long histories leave the card idle: 1,024
+// lone wavefronts, ranges of 256 keys or more (one query of 8 heads of 64 over 100,000 keys, bf16: all
+// gradients 4,120 us without, 274 with).
+int q_splits(const Args &a) {
+    const int64_t tiles = (a.Nq / 32 + a.B) * a.H;
+    if (a.B < 1 || tiles >= 512 || a.Nk < 1024 * a.B || a.Nq * 4 > a.Nk) return 1;
+    const int64_t s = 1024 / tiles, most = a.Nk / a.B / 256;
+    return static_cast<int>(s < most ? s : most);
+}
 int64_t key_tiles(const Args &a) { return a.Nk / 128 + 1; }
 
 // dT[b, h] from the workgroups' shares [slots, H, buckets], in a fixed order: every
@@ -497,18 +527,24 @@ template <typename T, int DP, int WAVES, int BK>
 int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     const Args &a = b.f;
     const int64_t nq = slots(a.Nq, a.B, 32 * WAVES), nk = slots(a.Nk, a.B, 32 * WAVES);
-    if (nq * a.H * 64 * WAVES > kMost || nk * a.Hkv * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
-    const int splits = WAVES == 1 ? 1 : kv_splits(a, key_tiles(a));
-    if (nk * a.Hkv * splits * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
+    const int splits = WAVES == 1 ? 1 : kv_splits(a, key_tiles(a)), qs = WAVES == 1 ? q_splits(a) : 1;
+    if (nq * a.H * qs * 64 * WAVES > kMost || nk * a.Hkv * splits * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
     Carver c(ws);
     float *delta = c.take<float>(a.Nq * a.H);
-    float *part = c.take<float>(b.grad_table ? nq * a.H * a.buckets : 0);
+    float *part = c.take<float>(b.grad_table ? nq * qs * a.H * a.buckets : 0);
     float *kv_part = c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
+    float *dq_part = c.take<float>(qs > 1 ? qs * a.Nq * a.H * a.D : 0);
     if (!b.grad_table) part = nullptr;
     const size_t pair = 2 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
-    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H), 64 * WAVES,
-                                 pair * (WAVES == 1 ? 1 : 2) + bias * (part ? 2 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(b, nq, delta, part);
+    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H * qs), 64 * WAVES,
+                                 pair * (WAVES == 1 ? 1 : 2) + bias * (part ? 2 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(
+        b, nq, delta, part, qs, dq_part);
     PYG_LAUNCH_CHECK();
+    if (qs > 1) {
+        const int64_t n = a.Nq * a.H * a.D;
+        k_join_q<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(dq_part, n, qs, static_cast<T *>(b.grad_q));
+        PYG_LAUNCH_CHECK();
+    }
     const size_t own = kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0;
     k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv * splits), 64 * WAVES,
                                   2 * pair + own + 8 * BK * sizeof(float) + bias, s>>>(b, nk, delta, splits, kv_part);
@@ -520,7 +556,7 @@ int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
         PYG_LAUNCH_CHECK();
     }
     if (part) {
-        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), 1024, 0, s>>>(part, nq, a.H, a.buckets,
+        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), 1024, 0, s>>>(part, nq * qs, a.H, a.buckets,
                                                                             static_cast<T *>(b.grad_table));
         PYG_LAUNCH_CHECK();
     }
@@ -548,7 +584,9 @@ int by_width(const BackwardArgs &b, void *ws, hipStream_t s) {
 size_t backward_workspace(const Args &a) {
     Carver c(nullptr);
     c.take<float>(a.Nq * a.H);
-    c.take<float>(slots(a.Nq, a.B, 32) * a.H * a.buckets);  // the smallest tiles have the most slots
+    const int qs = q_splits(a);
+    c.take<float>(slots(a.Nq, a.B, 32) * qs * a.H * a.buckets);  // the smallest tiles have the most slots
+    c.take<float>(qs > 1 ? qs * a.Nq * a.H * a.D : 0);
     const int splits = kv_splits(a, key_tiles(a));
     c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
     return align_up(c.used, 256);

@@ -94,8 +94,8 @@ def _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, zero_rest) ->
             raise ValueError("buckets must be [2 * reach + 1]")
     _same_device(q.device, k=k, v=v, ptr=ptr, k_ptr=k_ptr, table=table, buckets=buckets)
     scale = D ** -0.5 if scale is None else float(scale)
-    if not 0.0 < scale <= 1e30:
-        raise ValueError("scale must be positive and finite")
+    if not 1e-30 <= scale <= 1e30:
+        raise ValueError("scale must lie between 1e-30 and 1e30")
     return _Attention(ptr.data_ptr(), k_ptr.data_ptr(), ptr.shape[0] - 1, Nq, Nk, H, Hkv, D, q.stride(0), q.stride(1),
                       k.stride(0), k.stride(1), v.stride(0), v.stride(1), DTYPE[q.dtype], scale, int(bool(causal)),
                       _ptr(table), _ptr(buckets), 0 if table is None else table.shape[0],

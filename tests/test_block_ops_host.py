@@ -1,0 +1,124 @@
+"""The transformer block's C entries without a GPU: bad arguments are refused on the
+host before any device work, and workspace queries answer for what is allowed."""
+import ctypes
+import os
+
+import pytest
+
+PYG_OK, INVALID, WORKSPACE, UNSUPPORTED = 0, -1, -3, -5
+A, B_, C_, D_ = (ctypes.c_void_p(0x100000 * i) for i in (1, 2, 3, 4))  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_1903_02428_amd as pyg
+    if not os.path.exists(pyg.library_path()):
+        from paper_1903_02428_amd import build
+        build.build()
+    return pyg.library()
+
+
+def attention(**change):
+    from paper_1903_02428_amd.binding import _Attention
+    a = dict(q_ptr=0x1000, k_ptr=0x1000, B=2, Nq=100, Nk=100, H=4, Hkv=2, D=32, q_row=128, q_head=32, k_row=64, k_head=32,
+             v_row=64, v_head=32, dtype=1, scale=0.2, causal=0, table=0x2000, bucket=0x3000, buckets=8, reach=16, zero_rest=1)
+    a.update(change)
+    return _Attention(*a.values())
+
+
+def size(fn, *args):
+    out = ctypes.c_size_t(0)
+    return fn(*args, ctypes.byref(out)), out.value
+
+
+def test_attention_refusals(lib):
+    def rc(a, q=A, out=D_, stat=None, rest=None, ws=A, nbytes=1 << 40):
+        return lib.pyg_global_attention(ctypes.byref(a) if a else None, q, B_, C_, out, stat, rest, ws, nbytes, None)
+    assert rc(None) == INVALID
+    for change in (dict(dtype=7), dict(B=-1), dict(Nq=-1), dict(H=0), dict(Hkv=3), dict(D=0), dict(scale=0.0), dict(scale=-1.0),
+                   dict(scale=float("nan")), dict(scale=float("inf")), dict(bucket=None), dict(buckets=0), dict(reach=-1),
+                   dict(q_ptr=None), dict(k_ptr=None), dict(q_row=0), dict(k_head=0), dict(v_row=32), dict(q_head=64)):
+        assert rc(attention(**change)) == INVALID, change
+    for change in (dict(D=129, q_head=129, q_row=600, k_head=129, k_row=300, v_head=129, v_row=300), dict(reach=1025), dict(buckets=1025),
+                   dict(Nq=1 << 31), dict(H=65536), dict(q_row=1 << 22)):
+        assert rc(attention(**change)) == UNSUPPORTED, change
+    assert rc(attention(), q=None) == INVALID and rc(attention(), out=None) == INVALID
+    assert rc(attention(dtype=0), rest=A) == INVALID  # nothing is rounded away in fp32
+    few = attention(Nq=2, Nk=100_000)
+    status, need = size(lib.pyg_global_attention_workspace, ctypes.byref(few))
+    assert status == PYG_OK and need >= 2 * 4 * (32 + 2) * 4
+    assert rc(few, nbytes=need - 1) == WORKSPACE and rc(few, ws=None) == WORKSPACE
+    assert size(lib.pyg_global_attention_workspace, ctypes.byref(attention(Nq=0))) == (PYG_OK, 0)
+    assert rc(attention(Nq=0), q=None, out=None) == PYG_OK  # nothing to do
+
+
+def test_attention_backward_refusals(lib):
+    a = attention()
+    status, need = size(lib.pyg_global_attention_backward_workspace, ctypes.byref(a))
+    assert status == PYG_OK and need >= 100 * 4 * 4
+
+    def rc(a=a, **change):
+        p = dict(g=A, q=A, k=B_, v=C_, out=A, stat=A, rest=None, gq=D_, gk=D_, gv=D_, gt=D_, ws=A, n=need)
+        p.update(change)
+        return lib.pyg_global_attention_backward(ctypes.byref(a), *p.values(), None)
+    for name in ("g", "q", "k", "v", "out", "stat", "gq", "gk", "gv"):
+        assert rc(**{name: None}) == INVALID, name
+    assert rc(attention(table=None), gt=D_) == INVALID
+    assert rc(n=need - 1) == WORKSPACE and rc(ws=None) == WORKSPACE
+
+
+def norm(**change):
+    from paper_1903_02428_amd.binding import _BlockNorm
+    a = dict(dtype=0, norm=0, N=10, F=64, eps=1e-5, h=0x1000, residual=0x2000, gate=None, gate_rows=0, scale=0x3000, post_weight=0x4000,
+             post_bias=0x5000, weight=0x6000, bias=0x7000)
+    a.update(change)
+    return _BlockNorm(*a.values())
+
+
+def test_block_norm_refusals(lib):
+    def rc(a, r=A, y=B_, codes=None, steps=None):
+        return lib.pyg_block_norm(ctypes.byref(a), r, y, codes, steps, None)
+    for change in (dict(dtype=3), dict(norm=2), dict(N=-1), dict(F=0), dict(eps=-1.0), dict(eps=float("nan")), dict(post_weight=None),
+                   dict(weight=None), dict(h=None)):
+        assert rc(norm(**change)) == INVALID, change
+    assert rc(norm(F=8193)) == UNSUPPORTED and rc(norm(N=1 << 31)) == UNSUPPORTED
+    assert rc(norm(), y=None) == INVALID and rc(norm(weight=None, bias=None), y=B_) == INVALID
+    assert rc(norm(), codes=A) == INVALID and rc(norm(weight=None, bias=None), y=None, codes=A, steps=B_) == INVALID
+    assert rc(norm(N=0), r=None, y=None) == PYG_OK
+    status, need = size(lib.pyg_block_norm_backward_workspace, ctypes.byref(norm()))
+    assert status == PYG_OK and need > 0
+
+    def back(a=norm(), gr=A, gy=B_, gate=None, scale=D_, n=need, ws=A):
+        return lib.pyg_block_norm_backward(ctypes.byref(a), gr, gy, C_, C_, gate, scale, D_, D_, D_, D_, ws, n, None)
+    assert back(gr=None, gy=None) == INVALID and back(gate=D_) == INVALID and back(norm(scale=None)) == INVALID
+    assert back(norm(weight=None, bias=None)) == INVALID
+    assert back(n=need - 1) == WORKSPACE and back(ws=None) == WORKSPACE
+
+
+def test_checkpoint_and_dense_refusals(lib):
+    ck = lib.pyg_activation_checkpoint
+    assert ck(A, 5, 4, 8, B_, C_, None) == INVALID and ck(A, 0, -1, 8, B_, C_, None) == INVALID and ck(A, 0, 4, 0, B_, C_, None) == INVALID
+    assert ck(None, 0, 4, 8, B_, C_, None) == INVALID and ck(A, 0, 4, 8, ctypes.c_void_p(0x1004), C_, None) == INVALID
+    assert ck(A, 0, 1 << 31, 8, B_, C_, None) == UNSUPPORTED and ck(None, 0, 0, 8, None, None, None) == PYG_OK
+    assert lib.pyg_checkpoint_restore(A, B_, 4, 8, None, 0, None) == INVALID
+    status, need = size(lib.pyg_dense_transform_backward_workspace, 0, 1000, 64, 32)
+    assert status == PYG_OK and need >= 64 * 32 * 4
+    assert size(lib.pyg_dense_transform_backward_workspace, 0, 1000, 0, 32)[0] == INVALID
+
+    def rc(dtype=0, N=1000, Fo=32, Fi=64, g=A, theta=B_, codes=C_, gx=D_, gt=D_, ws=A, n=need):
+        return lib.pyg_dense_transform_backward(g, dtype, N, Fo, theta, Fi, codes, C_, gx, gt, ws, n, None)
+    assert rc(dtype=2) == INVALID and rc(g=None) == INVALID and rc(theta=None) == INVALID and rc(codes=None) == INVALID
+    assert rc(codes=ctypes.c_void_p(0x1008)) == INVALID and rc(Fi=1 << 24) == UNSUPPORTED
+    assert rc(n=need - 1) == WORKSPACE and rc(ws=None) == WORKSPACE
+
+
+def test_relative_buckets():
+    import paper_1903_02428_amd as pyg
+    t = pyg.relative_buckets(8, 16, True, "cpu").tolist()
+    assert t[16] == 0 and t[15] == 1 and t[17] == 5 and t[0] == 3 and t[-1] == 7  # own buckets for later keys
+    assert sorted(set(t)) == [0, 1, 2, 3, 5, 6, 7]  # no later key at distance 0
+    t = pyg.relative_buckets(8, 32, False, "cpu").tolist()
+    assert t[33:] == [0] * 32 and t[:33][::-1] == sorted(t[:33]) and t[0] == 7
+    for bad in ((1, 8, True), (8, 2, True), (7, 8, True), (0, 8, False)):
+        with pytest.raises(ValueError):
+            pyg.relative_buckets(*bad, "cpu")

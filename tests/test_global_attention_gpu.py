@@ -57,6 +57,9 @@ CASES = [
     ([1], [5000], 16, 2, 128, 32, 128, False),
     ([2], [2049], 1, 1, 24, 0, 0, True),
     ([1, 17], [100, 31], 20, 1, 40, 4, 8, False),
+    # more of them over a long history: several tiles of 16 rows, and many heads on one key head
+    ([40, 3], [2600, 90], 2, 1, 64, 8, 16, True),
+    ([1], [1500], 40, 1, 32, 8, 64, True),
     # small graphs: a wavefront each
     ([25, 1, 32, 33, 0, 18], None, 4, 4, 16, 16, 32, False),
     ([40, 20, 7], None, 8, 8, 8, 8, 16, True),
@@ -249,7 +252,7 @@ def test_refusals(pyg):
            dict(k=x[:5], v=x[:5]), dict(k=x.bfloat16(), v=x.bfloat16()), dict(q=x.transpose(1, 2)), dict(ptr=ptr.int()),
            dict(k_ptr=ptr_of([3, 3])), dict(table=table), dict(buckets=lut), dict(table=table[:, :2].contiguous(), buckets=lut),
            dict(table=table.bfloat16(), buckets=lut), dict(table=table, buckets=lut[1:]), dict(table=table, buckets=lut.long()),
-           dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(out=x[:3]), dict(out=x.bfloat16()),
+           dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=1e-31), dict(out=x[:3]), dict(out=x.bfloat16()),
            dict(stat=torch.zeros(6, 4, device="cuda")), dict(rest=x)]
     for change in bad:
         with pytest.raises(ValueError):
@@ -262,6 +265,8 @@ def test_refusals(pyg):
     far = torch.zeros(2 * 1025 + 1, dtype=torch.int32, device="cuda")
     with pytest.raises(pyg.PygError):
         pyg.global_attention(x, x, x, ptr, None, table, far)
+    with pytest.raises(pyg.PygError):
+        pyg.global_attention(x, x, x, ptr, out=x)  # over its own input
     same = x[:1].expand(6, 4, 8)  # one row six times: rows overlap
     with pytest.raises(pyg.PygError):
         pyg.global_attention(x, same, same, ptr)
