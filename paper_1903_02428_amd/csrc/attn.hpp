@@ -61,14 +61,6 @@ __device__ __forceinline__ bool stage_bias(const Args &a, int h, float *bias, in
     return __syncthreads_or(wild) != 0;
 }
 
-// A part of a kernel that comes in two forms: the inner one, for tiles that no mask, end or
-// varying bias touches, has no branches, so that its products and exponentials overlap.
-struct Inner {
-    static constexpr bool value = true;
-};
-struct Edge {
-    static constexpr bool value = false;
-};
 // Whether the offsets first .. last all lie in an end bucket, and none is masked.
 __device__ __forceinline__ bool flat(int first, int last, int reach, bool causal) {
     return last <= -reach || (first >= reach && !causal);

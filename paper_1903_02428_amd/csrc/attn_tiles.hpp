@@ -296,11 +296,11 @@ struct Place {
     int64_t tile;                // which of its tiles
 };
 
-// mul: rows of the batch count `mul` times (query rows of several heads in one tile).
 __device__ __forceinline__ int64_t ptr_at(const int64_t *__restrict__ ptr, int64_t g, int64_t N) {
     const int64_t v = ptr[g];
     return v < 0 ? 0 : v > N ? N : v;
 }
+// Where a slot lies. mul: rows of the batch count `mul` times (query rows of several heads in one tile).
 __device__ __forceinline__ Place place_of(const int64_t *__restrict__ ptr, int64_t B, int64_t N, int64_t slot, int tile,
                                           int mul, int lane) {
     int64_t lo = 0, hi = B + 1;  // graph lo's slots start at or before `slot`, graph hi's after it
