@@ -56,8 +56,8 @@ struct FewTile {
                                          int64_t end, int lane) {
         const int m = lane & 15, g = lane >> 4;
         if (a.D % F::E == 0 && a.D % F::W == 0) {
-            // without a branch, so that all loads are under way together: keys past the end are the last one again (their
-            // weight is 0), features past D the first ones (Q is 0 there, or the result is not kept)
+            // without a branch, so that all loads are under way together: keys past the end are the last one again,
+            // features past D the first ones; clear() takes them out where they would count
             const int64_t last = end - 1;
             const int d = m * F::W < a.D ? m * F::W : 0;
 #pragma unroll
@@ -92,6 +92,27 @@ struct FewTile {
                 k[u][s] = load_piece<T>(kb + key * a.k_row, 4 * F::E * s + F::E * g, a.D, key < end);
 #pragma unroll
             for (int r = 0; r < 4; ++r) row(a, vb, j + 16 * u + 4 * g + r, end, m, v[4 * u + r]);
+        }
+    }
+    // What load() put in the place of nothing, to zeros before it is used: 0 times an infinity would be NaN. (K past the
+    // end is masked, features of V past D are not kept.)
+    __device__ __forceinline__ void clear(const Args &a, int64_t j, int64_t end, int lane) {
+        const int g = lane >> 4;
+        if (a.D < DP) {
+#pragma unroll
+            for (int s = 0; s < F::STEPS; ++s)
+                if (4 * F::E * s + F::E * g >= a.D)
+#pragma unroll
+                    for (int u = 0; u < F::SUB; ++u) k[u][s] = make_uint4(0, 0, 0, 0);
+        }
+        if (j + F::KEYS > end) {
+#pragma unroll
+            for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (j + 16 * u + 4 * g + r >= end)
+#pragma unroll
+                        for (int i = 0; i < F::VW; ++i) v[4 * u + r][i] = 0;
         }
     }
     __device__ __forceinline__ void row(const Args &a, const T *__restrict__ vb, int64_t key, int64_t end, int m,
@@ -183,6 +204,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
     if (j < end) cur.load(a, kb, vb, j, end, lane);
     for (; j < end; j += kFewWaves * F::KEYS) {
         if (j + kFewWaves * F::KEYS < end) next.load(a, kb, vb, j + kFewWaves * F::KEYS, end, lane);
+        cur.clear(a, j, end, lane);
         f32x4 s[F::SUB];
         // all offsets of the tile at or below -reach, for all of the wavefront's rows
         const bool is_far = j + F::KEYS - 1 - (r0 / a.G + nk - nq) <= -a.reach;
@@ -319,11 +341,12 @@ __global__ __launch_bounds__(kBlock) void k_join(const Args a, int splits, const
         }
         for (int s = 0; s < n; s += 8) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {  // past the last range the weight is 0
+            for (int i = 0; i < 8; ++i) {  // past the last range the weight is 0, and what stands there may be infinite
                 const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s + i));
                 const float *o = x + (s + i < n ? s + i : n - 1) * (a.D + 2) + 2;
-                o0 = fmaf(ws, o[d0], o0);
-                o1 = fmaf(ws, o[d1], o1);
+                const float x0 = o[d0], x1 = o[d1];
+                o0 = fmaf(ws, s + i < n ? x0 : 0.f, o0);
+                o1 = fmaf(ws, s + i < n ? x1 : 0.f, o1);
             }
         }
     }

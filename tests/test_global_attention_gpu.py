@@ -270,3 +270,34 @@ def test_refusals(pyg):
     same = x[:1].expand(6, 4, 8)  # one row six times: rows overlap
     with pytest.raises(pyg.PygError):
         pyg.global_attention(x, same, same, ptr)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [8, 16, 24, 80, 128])
+def test_few_queries_infinite_keys(pyg, D, dtype):
+    """A key whose score is -infinity counts for nothing, whatever width its features are padded to: the
+    result is that of the keys without it. One query a graph, in one range of keys and in several."""
+    for qn, kn in (([1, 1], [40, 300]), ([1], [5000])):
+        q, k, v, _, _, _ = inputs(11, qn, kn, 4, 2, D, DT[dtype], 0, 0, False, pyg)
+        q[:, :, 0] = q[:, :, 0].abs() + 0.5
+        at = [0, 7, sum(kn) - 1] + ([39, 40] if len(kn) > 1 else [])  # the first and last keys of the graphs too
+        k[at, :, 0] = -math.inf
+        keep = torch.ones(sum(kn), dtype=torch.bool)
+        keep[at] = False
+        left = [int(n.sum()) for n in keep.split(kn)]
+        out = pyg.global_attention(q.cuda(), k.cuda(), v.cuda(), ptr_of(qn), ptr_of(kn))
+        close({"out": out}, attention(q, k[keep], v[keep], qn, left), f"{D} {dtype} {kn}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [16, 24, 128])
+def test_few_queries_infinite_values(pyg, D, dtype):
+    """An infinite feature of the last key's value makes that feature of the result infinite, and no other."""
+    for qn, kn in (([1, 1], [37, 301]), ([1], [5001])):
+        q, k, v, _, _, _ = inputs(12, qn, kn, 4, 2, D, DT[dtype], 0, 0, False, pyg)
+        ref = attention(q, k, v, qn, kn)
+        v[sum(kn) - 1, 1, 3] = math.inf  # key head 1: query heads 2 and 3
+        out = pyg.global_attention(q.cuda(), k.cuda(), v.cuda(), ptr_of(qn), ptr_of(kn)).cpu()
+        assert (out[-1, 2:, 3] == math.inf).all(), out[-1, 2:, 3]
+        out[-1, 2:, 3] = ref["out"][0][-1, 2:, 3].to(out.dtype)
+        close({"out": out}, ref, f"{D} {dtype} {kn}")
