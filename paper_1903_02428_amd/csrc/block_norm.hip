@@ -213,9 +213,9 @@ struct Body {
 };
 
 // exp and reciprocal by the hardware's instructions, each within one step of fp32 (and the exponent's rounding)
-__device__ __forceinline__ float sigmoid(float x) {
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x));
-}
+__device__ __forceinline__ float sigmoid_of(float e) { return __builtin_amdgcn_rcpf(1.f + e); }  // e = exp(-x)
+__device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(-1.4426950408889634f * x); }
+__device__ __forceinline__ float sigmoid(float x) { return sigmoid_of(exp_minus(x)); }
 
 template <typename T, int L, int NV>
 __global__ __launch_bounds__(threads_of(L)) void k_block_norm(const Norm a) {
@@ -342,14 +342,16 @@ __global__ __launch_bounds__(threads_of(L)) void k_block_norm_grad(const Norm a)
     if (kRoom && row < a.N) fetch(row);
     for (; row < a.N; row += step) {
         if (!kRoom) fetch(row);
-        float nh[M], sg[M], nr[M], t[M], p[M], gy[M];
+        float nh[M], ge[M], nr[M], t[M], p[M], gy[M];
         B::open(rh, nh);
         B::open(rr, nr);
-        B::open(rg, sg);
+        B::open(rg, ge);
         B::open(ry, gy);
         B::open(rt, t);
-        float gr = 1.f;
-        if (a.gate && a.gate_rows) gr = sigmoid(static_cast<float>(static_cast<const T *>(a.gate)[row]));
+        // the gate as e = exp(-x): sigmoid(x) = 1 / (1 + e), sigmoid(-x) = e sigmoid(x), each with all its bits (1 - sigmoid(x)
+        // would lose them from logits of about 12 on)
+        float gr = 0.f;
+        if (a.gate && a.gate_rows) gr = exp_minus(static_cast<float>(static_cast<const T *>(a.gate)[row]));
         if (kRoom && row + step < a.N) fetch(row + step);  // on its way while this row is worked on
         float rstd_h = 0.f;
         if (a.post) rstd_h = B::normalise(nh, a, lane, lds);
@@ -366,8 +368,8 @@ __global__ __launch_bounds__(threads_of(L)) void k_block_norm_grad(const Norm a)
         }
 #pragma unroll
         for (int k = 0; k < M; ++k) {
-            sg[k] = !a.gate ? 1.f : a.gate_rows ? gr : sigmoid(sg[k]);
-            const float c = sc[k] * sg[k] * u[k];
+            ge[k] = !a.gate || a.gate_rows ? gr : exp_minus(ge[k]);
+            const float c = sc[k] * sigmoid_of(ge[k]) * u[k];
             nr[k] = !B::inside(lane, k, a.F) ? 0.f : a.residual ? nr[k] + c : c;
             if (!a.grad_r) t[k] = 0.f;
         }
@@ -389,11 +391,14 @@ __global__ __launch_bounds__(threads_of(L)) void k_block_norm_grad(const Norm a)
         float dg[M], row_gate[1] = {0.f};
 #pragma unroll
         for (int k = 0; k < M; ++k) {
-            s_sc[k] = fmaf(t[k] * sg[k], u[k], s_sc[k]);
+            // made again where registers are short, not kept beside e
+            if constexpr (!kRoom) asm volatile("" : "+v"(ge[k]));
+            const float g = sigmoid_of(ge[k]);
+            s_sc[k] = fmaf(t[k] * g, u[k], s_sc[k]);
             t[k] *= sc[k];
-            dg[k] = t[k] * u[k] * sg[k] * (1.f - sg[k]);
+            dg[k] = t[k] * u[k] * g * (fminf(ge[k], 0x1p126f) * g);  // e beyond 2^126: g is 0
             row_gate[0] += dg[k];
-            t[k] *= sg[k];  // the gradient of u
+            t[k] *= g;  // the gradient of u
         }
         if (a.grad_gate) {
             if (a.gate_rows) {

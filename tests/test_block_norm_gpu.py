@@ -226,3 +226,25 @@ def test_refusals(pyg):
         pyg.block_norm_backward(None, None, x, weight=w)
     with pytest.raises(ValueError):
         pyg.block_norm_backward(None, x, x)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [False, True])
+def test_gate_gradient_far_from_zero(pyg, rows, dtype):
+    """d sigmoid = sigmoid(x) sigmoid(-x) keeps its bits where sigmoid(x) is nearly one. Of all-positive
+    terms: the exponent's argument x log2 e is off by two half steps (the constant's and the product's rounding), so
+    each of the two factors by 2 |x| half steps at most; exp2, the reciprocal (a whole step each) and
+    the sum in each, the other products and a row's sum of F terms are the rest."""
+    F = 24
+    x = torch.tensor([-80.0, -40, -17, -12, -3, 0, 3, 8, 12, 15, 17, 20, 25, 40, 60, 80])
+    g = torch.Generator().manual_seed(5)
+    h, gr = (torch.rand(len(x), F, generator=g).to(DT[dtype]) + 0.5 for _ in range(2))
+    gate = (x[:, None] if rows else x[:, None].expand(-1, F)).contiguous().to(DT[dtype])
+    scale = torch.rand(F, generator=g) + 0.5
+    got = pyg.block_norm_backward(gr.cuda(), None, h.cuda(), gate=gate.cuda(), scale=scale.cuda())[2].cpu().double()
+    xd = gate.double()
+    want = gr.double() * scale.double() * h.double() * torch.sigmoid(xd) * torch.sigmoid(-xd)
+    want = want.sum(1, keepdim=True) if rows else want
+    half = 0.0 if dtype == "f32" else torch.finfo(torch.bfloat16).eps / 2
+    bound = ((4 * xd.abs() + 16 + (F if rows else 0)) * U + half) * want
+    assert ((got - want).abs() <= bound).all(), ((got - want).abs() / bound).amax(1)
