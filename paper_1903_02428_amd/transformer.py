@@ -27,6 +27,14 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} must be on {device}, got {t.device}")
 
 
+def _written(*tensors):
+    """Kernels write through addresses, which autograd does not see: a caller's tensor that was written
+    counts as modified in place, so that a backward that kept it says so."""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def relative_buckets(num_buckets: int = 32, max_distance: int = 128, bidirectional: bool = True,
                      device="cuda") -> torch.Tensor:
     """Bucket of every offset -max_distance .. max_distance (key position minus
@@ -132,7 +140,7 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
     get zeros, but are left as they were in an `out` that the caller brings."""
     lib = library()
     c = _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, out is None)
-    dev = q.device
+    dev, given = q.device, out
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     else:
@@ -151,6 +159,7 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
             workspace = _workspace(nbytes, dev)
         _check(lib.pyg_global_attention(ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(stat),
                                         _ptr(rest), _ptr(workspace), nbytes, _stream(dev)), "pyg_global_attention")
+    _written(given, stat, rest)
     return out
 
 
@@ -268,6 +277,7 @@ def activation_checkpoint(x: torch.Tensor, out: Checkpoint | None = None) -> Che
     N, F = x.shape
     if F < 1:
         raise ValueError("x must have features")
+    given = out
     if out is None:
         out = _new_checkpoint(N, F, x.dtype, x.device)
     elif (out.N, out.F, out.dtype) != (N, F, x.dtype):
@@ -276,6 +286,8 @@ def activation_checkpoint(x: torch.Tensor, out: Checkpoint | None = None) -> Che
     with _on(x.device):
         _check(library().pyg_activation_checkpoint(_ptr(x), DTYPE[x.dtype], N, F, _ptr(out.codes), _ptr(out.steps),
                                                    _stream(x.device)), "pyg_activation_checkpoint")
+    if given is not None:
+        _written(given.codes, given.steps)
     return out
 
 
@@ -285,7 +297,7 @@ def checkpoint_restore(kept: Checkpoint, dtype: torch.dtype | None = None, out: 
     dtype = (kept.dtype if out is None else out.dtype) if dtype is None else dtype
     if dtype not in DTYPE:
         raise ValueError("dtype must be float32 or bfloat16")
-    dev = kept.codes.device
+    dev, given = kept.codes.device, out
     if out is None:
         out = torch.empty((kept.N, kept.F), dtype=dtype, device=dev)
     else:
@@ -296,6 +308,7 @@ def checkpoint_restore(kept: Checkpoint, dtype: torch.dtype | None = None, out: 
     with _on(dev):
         _check(library().pyg_checkpoint_restore(_ptr(kept.codes), _ptr(kept.steps), kept.N, kept.F, _ptr(out),
                                                 DTYPE[dtype], _stream(dev)), "pyg_checkpoint_restore")
+    _written(given)
     return out
 
 

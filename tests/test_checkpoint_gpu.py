@@ -137,3 +137,30 @@ def test_empty_and_refusals(pyg):
             pyg.dense_transform_backward(*args)
     with pytest.raises(ValueError):
         pyg.checkpoint_restore(kept, torch.float16)
+
+
+def test_written_again_is_noticed(pyg):
+    """Arrays that autograd holds and a call writes again: the backward says so and does not use the new values."""
+    x = torch.randn(40, 64, device="cuda")
+    theta = torch.randn(64, 8, device="cuda", requires_grad=True)
+    kept = pyg.activation_checkpoint(x)
+    out = pyg.DenseTransform.apply(x, theta, kept)
+    pyg.activation_checkpoint(2 * x, out=kept)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out, [theta], torch.ones_like(out))
+    out = pyg.DenseTransform.apply(x, theta, kept)  # and of what is there now it is right
+    want = pyg.dense_transform_backward(torch.ones_like(out), theta.detach(), kept, need_grad_x=False)[1]
+    assert torch.equal(torch.autograd.grad(out, [theta], torch.ones_like(out))[0], want)
+    saved = torch.randn(40, 64, device="cuda", requires_grad=True).exp()
+    pyg.checkpoint_restore(kept, out=saved.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(saved, [saved.grad_fn.next_functions[0][0].variable], torch.ones_like(saved))
+    saved = torch.randn(5, 2, 8, device="cuda", requires_grad=True).exp()
+    qkv = torch.randn(5, 2, 8, device="cuda")
+    pyg.global_attention(qkv, qkv, qkv, torch.tensor([0, 5], device="cuda"), out=saved.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(saved, [saved.grad_fn.next_functions[0][0].variable], torch.ones_like(saved))
+    with torch.inference_mode():  # arrays without versions are written as they are
+        kept = pyg.activation_checkpoint(x)
+        pyg.activation_checkpoint(x, out=kept)
+        pyg.checkpoint_restore(kept, out=torch.empty_like(x))
