@@ -840,8 +840,9 @@ int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int
  *   grad_theta [Fi, Fo] = X^T G with X from codes and steps (NULL with grad_theta NULL);
  *   grad_x     [N, Fi]  = G Theta^T (theta [Fi, Fo] row-major, or NULL with grad_x NULL);
  * G = grad_out [N, Fo], theta and both results in dtype, fp32 accumulation. fp32
- * operands enter the matrix cores as three bf16 parts each, which hold all their bits
- * (magnitudes from 2^-100 on; an infinity of G or theta may come out of grad_x as NaN).
+ * operands enter the matrix cores as three bf16 parts each, which add up to them exactly
+ * (magnitudes from 2^-100 on). The products of grad_theta are exact; those of grad_x are off by less than
+ * 2^-24 of themselves, to either side (an infinity of G or theta may come out of grad_x as NaN).
  * Deterministic. Errors: PYG_ERR_INVALID_ARG, PYG_ERR_UNSUPPORTED (N >= 2^31, Fi or Fo >=
  * 2^24), PYG_ERR_WORKSPACE. */
 int pyg_dense_transform_backward(const void *grad_out, int dtype, int64_t N, int64_t Fo, const void *theta, int64_t Fi,

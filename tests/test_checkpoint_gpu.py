@@ -164,3 +164,38 @@ def test_written_again_is_noticed(pyg):
         kept = pyg.activation_checkpoint(x)
         pyg.activation_checkpoint(x, out=kept)
         pyg.checkpoint_restore(kept, out=torch.empty_like(x))
+
+
+def test_input_gradient_of_single_products(pyg):
+    """fp32 grad_x of one term a value is the product itself to within the matrix cores' last addition: operands as
+    three bf16 parts each, the part products that are left out below 2^-24 of the whole (half a step
+    of fp32), the six that are taken exact, summed from the smallest on: one step (two half steps,
+    should the sum be cut and not rounded) for the last addition, at most half of one half step for those before."""
+    g = torch.Generator().manual_seed(9)
+    bits = (torch.randint(0, 1 << 23, (1500 + 300,), generator=g, dtype=torch.int32) | 0x3F800000)
+    bits[:8] = bits[1500:1508] = torch.tensor([0x3F80FFFF, 0x3F808000, 0x3F807FFF, 0x3F800001, 0x3FFFFFFF, 0x3FFF7FFF, 0x3F8080FF, 0x3F800000],
+                                              dtype=torch.int32)
+    val = bits.view(torch.float32)
+    sign = torch.where(torch.rand(len(val), generator=g) < 0.5, -1.0, 1.0)
+    go, theta = (val * sign)[:1500, None].contiguous(), (val * sign)[1500:, None].contiguous()
+    gx, _ = pyg.dense_transform_backward(go.cuda(), theta.cuda(), None, need_grad_theta=False)
+    want = go.double() @ theta.double().T
+    err = (gx.cpu().double() - want).abs() / want.abs()
+    assert float(err.max()) <= 3.5 * U, f"{float(err.max() / U):.2f} half steps"
+
+
+def test_parts_of_extreme_values(pyg):
+    """Cutting fp32 operands into parts keeps the largest values finite, and NaN whatever its bits."""
+    top = torch.finfo(torch.float32).max
+    go = torch.tensor([top, -top, 3.4e38, 1.0, 0.0, 2.0 ** -90])[:, None]
+    theta = torch.ones(4, 1)
+    gx, _ = pyg.dense_transform_backward(go.cuda(), theta.cuda(), None, need_grad_theta=False)
+    assert torch.equal(gx.cpu(), go.expand(6, 4))
+    nan = torch.tensor([0x7F800001, -0x007FFFFF, 0x7FC00000], dtype=torch.int32).view(torch.float32)[:, None].contiguous()
+    assert torch.isnan(nan).all()
+    gx, _ = pyg.dense_transform_backward(nan.cuda(), theta.cuda(), None, need_grad_theta=False)
+    assert torch.isnan(gx).all()
+    x = torch.ones(3, 32)
+    _, gt = pyg.dense_transform_backward(torch.cat([nan[:1], torch.ones(2, 1)]).cuda(), torch.ones(32, 1, device="cuda"),
+                                         pyg.activation_checkpoint(x.cuda()))
+    assert torch.isnan(gt).all()
