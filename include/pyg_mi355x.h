@@ -759,11 +759,9 @@ int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
  * gives zeros, and zero gradients. Scores, sums and statistics are fp32; bf16
  * weights p are rounded to bf16 for the second product. Deterministic.
  * Errors: PYG_ERR_INVALID_ARG (NULL or negative or inconsistent arguments,
- * Hkv not dividing H, scale not in [1e-30, 1e30], overlapping strides, results that overlap
- * the inputs),
- * PYG_ERR_UNSUPPORTED (D > 128, reach or buckets > 1024, rows >= 2^31, row
- * strides >= 2^22 elements, a grid
- * beyond 2^32 threads), PYG_ERR_WORKSPACE. */
+ * Hkv not dividing H, scale not in [1e-30, 1e30], overlapping strides, results or a workspace that
+ * overlap the inputs or one another), PYG_ERR_UNSUPPORTED (D > 128, H > 65535, reach or buckets > 1024,
+ * rows >= 2^31, row strides >= 2^22 elements, a grid beyond 2^32 threads), PYG_ERR_WORKSPACE. */
 int pyg_global_attention(const pyg_attention *a, const void *q, const void *k, const void *v, void *out, float *stat,
                          void *rest, void *ws, size_t ws_bytes, void *stream);
 

@@ -39,6 +39,28 @@ struct Carver {
     }
 };
 
+// Bytes of memory that a call reads or writes (none: a NULL or nothing to read).
+struct Span {
+    const void *p;
+    int64_t bytes;
+};
+// Whether no result of a call meets one of its inputs or another of its results.
+template <int R, int I>
+static inline bool apart(const Span (&results)[R], const Span (&inputs)[I]) {
+    const auto meet = [](const Span &x, const Span &y) {
+        if (!x.p || !y.p || x.bytes <= 0 || y.bytes <= 0) return false;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+        return a < b ? b - a < static_cast<uintptr_t>(x.bytes) : a - b < static_cast<uintptr_t>(y.bytes);
+    };
+    for (int i = 0; i < R; ++i) {
+        for (int j = 0; j < I; ++j)
+            if (meet(results[i], inputs[j])) return false;
+        for (int j = 0; j < i; ++j)
+            if (meet(results[i], results[j])) return false;
+    }
+    return true;
+}
+
 static inline unsigned grid_for(int64_t work, int64_t per_block, int64_t cap = 1 << 20) {
     int64_t g = (work + per_block - 1) / per_block;
     if (g < 1) g = 1;

@@ -265,17 +265,22 @@ int take_inputs(const pyg_attention *c, const void *q, const void *k, const void
     return PYG_OK;
 }
 
-// Whether n elements at p meet the N rows of H heads at x.
-bool meets(const void *p, int64_t n, const void *x, int64_t N, int64_t H, int64_t D, int64_t row, int64_t head, size_t e) {
-    if (!p || !x || n <= 0 || N <= 0) return false;
-    const uintptr_t p0 = reinterpret_cast<uintptr_t>(p), x0 = reinterpret_cast<uintptr_t>(x);
-    const uintptr_t span = static_cast<uintptr_t>(row * (N - 1) + head * (H - 1) + D) * e;
-    return p0 < x0 + span && x0 < p0 + static_cast<uintptr_t>(n) * e;
+// Bytes from the first to the last of N rows of H heads of D features.
+int64_t span(int64_t N, int64_t H, int64_t D, int64_t row, int64_t head, size_t e) {
+    return N < 1 ? 0 : static_cast<int64_t>((row * (N - 1) + head * (H - 1) + D) * e);
 }
-bool meets_inputs(const pyg_attention *c, const Args &a, const void *p, int64_t n) {
-    const size_t e = bytes_of(c);
-    return meets(p, n, a.q, a.Nq, a.H, a.D, a.q_row, a.q_head, e) || meets(p, n, a.k, a.Nk, a.Hkv, a.D, a.k_row, a.k_head, e) ||
-           meets(p, n, a.v, a.Nk, a.Hkv, a.D, a.v_row, a.v_head, e);
+// What both directions read.
+struct Inputs {
+    Span s[7];
+};
+Inputs inputs_of(const Args &a, size_t e) {
+    return {{{a.q, span(a.Nq, a.H, a.D, a.q_row, a.q_head, e)},
+             {a.k, span(a.Nk, a.Hkv, a.D, a.k_row, a.k_head, e)},
+             {a.v, span(a.Nk, a.Hkv, a.D, a.v_row, a.v_head, e)},
+             {a.q_ptr, static_cast<int64_t>((a.B + 1) * sizeof(int64_t))},
+             {a.k_ptr, static_cast<int64_t>((a.B + 1) * sizeof(int64_t))},
+             {a.table, static_cast<int64_t>(a.buckets * a.H * e)},
+             {a.lut, static_cast<int64_t>((2 * a.reach + 1) * sizeof(int32_t))}}};
 }
 
 }  // namespace
@@ -305,8 +310,10 @@ extern "C" int pyg_global_attention(const pyg_attention *c, const void *q, const
     PYG_TRY(pyg_global_attention_workspace(c, &need));
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     if (a.Nq == 0) return PYG_OK;
-    if (meets_inputs(c, a, out, a.Nq * a.H * a.D) || meets_inputs(c, a, rest, a.Nq * a.H * a.D)) return PYG_ERR_INVALID_ARG;
     if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
+    const int64_t n = a.Nq * a.H * a.D, e = bytes_of(c);
+    const Span results[] = {{out, n * e}, {rest, n * e}, {stat, a.Nq * a.H * 8}, {ws, static_cast<int64_t>(need)}};
+    if (!apart(results, inputs_of(a, e).s)) return PYG_ERR_INVALID_ARG;
     a.out = out, a.stat = stat, a.rest = rest;
     a.vec_o = vectors(out, a.D, a.D, a.D, bytes_of(c)) && vectors(rest, a.D, a.D, a.D, bytes_of(c));
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -332,12 +339,13 @@ extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void 
     if (a.Nq > 0 && (!grad_out || !out || !stat || !grad_q)) return PYG_ERR_INVALID_ARG;
     if (a.Nk > 0 && (!grad_k || !grad_v)) return PYG_ERR_INVALID_ARG;
     if (grad_table && !c->table) return PYG_ERR_INVALID_ARG;
-    if (meets_inputs(c, a, grad_q, a.Nq * a.H * a.D) || meets_inputs(c, a, grad_k, a.Nk * a.Hkv * a.D) ||
-        meets_inputs(c, a, grad_v, a.Nk * a.Hkv * a.D))
-        return PYG_ERR_INVALID_ARG;
     const size_t need = attn::backward_workspace(a);
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
+    const int64_t e = bytes_of(c), nq = a.Nq * a.H * a.D * e, nk = a.Nk * a.Hkv * a.D * e;
+    const Span results[] = {{grad_q, nq}, {grad_k, nk}, {grad_v, nk}, {grad_table, a.buckets * a.H * e}, {ws, static_cast<int64_t>(need)}};
+    const Span kept[] = {{grad_out, nq}, {out, nq}, {rest, nq}, {stat, a.Nq * a.H * 8}};
+    if (!apart(results, inputs_of(a, e).s) || !apart(results, kept)) return PYG_ERR_INVALID_ARG;
     a.out = const_cast<void *>(out), a.stat = const_cast<float *>(stat), a.rest = const_cast<void *>(rest);
     b.grad_out = grad_out, b.grad_q = grad_q, b.grad_k = grad_k, b.grad_v = grad_v, b.grad_table = grad_table;
     a.vec_o = true;

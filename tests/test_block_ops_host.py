@@ -122,3 +122,44 @@ def test_relative_buckets():
     for bad in ((1, 8, True), (8, 2, True), (7, 8, True), (0, 8, False)):
         with pytest.raises(ValueError):
             pyg.relative_buckets(*bad, "cpu")
+
+
+def at(address):
+    return ctypes.c_void_p(address)
+
+
+def test_attention_overlaps(lib):
+    """Results that share a byte with an input, another result or the workspace are refused; so
+    every pair is, in both directions (nothing here reaches a device: the call ends at the check)."""
+    M = 1 << 30
+    few = attention(Nq=2, Nk=100_000)
+    need = size(lib.pyg_global_attention_workspace, ctypes.byref(few))[1]
+    base = dict(q=M, k=2 * M, v=3 * M, out=4 * M, stat=5 * M, rest=6 * M, ws=7 * M)
+    last = dict(q=2 * 128 * 2 - 2, k=100_000 * 64 * 2 - 2, out=2 * 128 * 2 - 2, stat=2 * 4 * 8 - 4, rest=2 * 128 * 2 - 2,
+                ws=need - 4)
+    last["v"] = last["k"]
+
+    def rc(p, a=few):
+        return lib.pyg_global_attention(ctypes.byref(a), *[at(p[n]) for n in ("q", "k", "v", "out", "stat", "rest", "ws")], need, None)
+    for r in ("out", "stat", "rest", "ws"):
+        for o in base:
+            if o != r:
+                assert rc({**base, r: base[o]}) == INVALID, (r, o)
+                assert rc({**base, r: base[o] + last[o]}) == INVALID, (r, o, "last")
+                assert rc({**base, r: base[o] - last[r]}) == INVALID, (r, o, "first")
+        for field in ("q_ptr", "k_ptr", "table", "bucket"):
+            assert rc({**base, r: M // 2}, attention(Nq=2, Nk=100_000, **{field: M // 2})) == INVALID, (r, field)
+
+    a = attention()
+    need = size(lib.pyg_global_attention_backward_workspace, ctypes.byref(a))[1]
+    names = ("g", "q", "k", "v", "out", "stat", "rest", "gq", "gk", "gv", "gt", "ws")
+    base = {n: (i + 1) * M for i, n in enumerate(names)}
+
+    def back(p, a=a):
+        return lib.pyg_global_attention_backward(ctypes.byref(a), *[at(p[n]) for n in names], need, None)
+    for r in ("gq", "gk", "gv", "gt", "ws"):
+        for o in names:
+            if o != r:
+                assert back({**base, r: base[o]}) == INVALID and back({**base, r: base[o] + 60}) == INVALID, (r, o)
+        for field in ("q_ptr", "k_ptr", "table", "bucket"):
+            assert back({**base, r: M // 2}, attention(**{field: M // 2})) == INVALID, (r, field)
