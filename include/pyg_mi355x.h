@@ -798,9 +798,9 @@ typedef struct {
 
 /* r and y [N, F] in dtype, each rounded once (y is taken of the unrounded r; r may be NULL
  * where y is made). codes and steps, or NULL: y as it was stored, in 8 bits (see
- * pyg_activation_checkpoint). Statistics are fp32, two-pass. Results may not overlap the inputs. Deterministic.
+ * pyg_activation_checkpoint). Statistics are fp32, two-pass. Deterministic.
  * Errors: PYG_ERR_INVALID_ARG (bad dtype or norm, missing arrays, y without weight or
- * weight without y, codes without y, eps < 0), PYG_ERR_UNSUPPORTED (F > 8192, N >= 2^31). */
+ * weight without y, codes without y, eps < 0, results that overlap the inputs or one another), PYG_ERR_UNSUPPORTED (F > 8192, N >= 2^31). */
 int pyg_block_norm(const pyg_block_norm_args *a, void *r, void *y, int8_t *codes, uint8_t *steps, void *stream);
 
 /* Workspace bytes needed by pyg_block_norm_backward. */
@@ -809,7 +809,7 @@ int pyg_block_norm_backward_workspace(const pyg_block_norm_args *a, size_t *byte
 /* Gradients from grad_r and grad_y [N, F] (either may be NULL: zeros): grad_h, grad_residual
  * [N, F], grad_gate in gate's shape, in dtype; grad_scale .. grad_bias fp32 [F]. NULL outputs
  * are not made. Nothing of the forward is kept: the rows are normalised again. Deterministic.
- * Errors: as above (a gradient of a part that is left out), PYG_ERR_WORKSPACE. */
+ * Errors: as above (a gradient of a part that is left out, a workspace over any array), PYG_ERR_WORKSPACE. */
 int pyg_block_norm_backward(const pyg_block_norm_args *a, const void *grad_r, const void *grad_y, void *grad_h,
                             void *grad_residual, void *grad_gate, float *grad_scale, float *grad_post_weight,
                             float *grad_post_bias, float *grad_weight, float *grad_bias, void *ws, size_t ws_bytes,

@@ -555,6 +555,16 @@ Norm fill(const pyg_block_norm_args *c) {
     return a;
 }
 
+// What both directions read.
+struct Inputs {
+    Span s[8];
+};
+Inputs inputs_of(const pyg_block_norm_args *c) {
+    const int64_t rows = c->N * (c->dtype == PYG_BF16 ? 2 : 4), all = rows * c->F, p = c->F * 4;
+    return {{{c->h, all}, {c->residual, all}, {c->gate, c->gate_rows ? rows : all}, {c->scale, p}, {c->post_weight, p},
+             {c->post_bias, p}, {c->weight, p}, {c->bias, p}}};
+}
+
 }  // namespace
 }  // namespace pyg
 
@@ -566,6 +576,9 @@ extern "C" int pyg_block_norm(const pyg_block_norm_args *c, void *r, void *y, in
     if (c->weight && !y && c->N > 0) return PYG_ERR_INVALID_ARG;
     if (c->N == 0) return PYG_OK;
     if (!c->h || (!r && !y)) return PYG_ERR_INVALID_ARG;
+    const int64_t all = c->N * c->F * (c->dtype == PYG_BF16 ? 2 : 4), blocks = c->N * ((c->F + 31) / 32);
+    const Span results[] = {{r, all}, {y, all}, {codes, blocks * 32}, {steps, blocks}};
+    if (!apart(results, inputs_of(c).s)) return PYG_ERR_INVALID_ARG;
     Norm a = fill(c);
     a.r = r, a.y = y, a.codes = codes, a.steps = steps;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -592,6 +605,11 @@ extern "C" int pyg_block_norm_backward(const pyg_block_norm_args *c, const void 
         return PYG_ERR_INVALID_ARG;
     const int64_t groups = grad_groups(c);
     if (ws_bytes < static_cast<size_t>(groups) * 5 * c->F * sizeof(float) || !ws) return PYG_ERR_WORKSPACE;
+    const int64_t rows = c->N * (c->dtype == PYG_BF16 ? 2 : 4), all = rows * c->F, p = c->F * 4;
+    const Span results[] = {{grad_h, all}, {grad_residual, all}, {grad_gate, c->gate_rows ? rows : all}, {grad_scale, p},
+                            {grad_post_weight, p}, {grad_post_bias, p}, {grad_weight, p}, {grad_bias, p}, {ws, groups * 5 * p}};
+    const Span grads[] = {{grad_r, all}, {grad_y, all}};
+    if (!apart(results, inputs_of(c).s) || !apart(results, grads)) return PYG_ERR_INVALID_ARG;
     Norm a = fill(c);
     a.grad_r = grad_r, a.grad_y = grad_y, a.grad_h = grad_h, a.grad_residual = grad_residual, a.grad_gate = grad_gate;
     a.part = static_cast<float *>(ws);

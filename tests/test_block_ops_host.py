@@ -163,3 +163,35 @@ def test_attention_overlaps(lib):
                 assert back({**base, r: base[o]}) == INVALID and back({**base, r: base[o] + 60}) == INVALID, (r, o)
         for field in ("q_ptr", "k_ptr", "table", "bucket"):
             assert back({**base, r: M // 2}, attention(**{field: M // 2})) == INVALID, (r, field)
+
+
+def test_block_norm_overlaps(lib):
+    M = 1 << 30
+    fields = ("h", "residual", "gate", "scale", "post_weight", "post_bias", "weight", "bias")
+    inputs = {n: (20 + i) * M for i, n in enumerate(fields)}
+    for gate_rows, gate_bytes in ((0, 10 * 64 * 4), (1, 10 * 4)):
+        a = norm(**inputs, gate_rows=gate_rows)
+        rows, par = 10 * 64 * 4, 64 * 4
+        length = {"h": rows, "residual": rows, "gate": gate_bytes, **{n: par for n in fields[3:]}, "r": rows, "y": rows, "codes": 640, "steps": 20}
+        base = {n: (i + 1) * M for i, n in enumerate(("r", "y", "codes", "steps"))}
+
+        def rc(p):
+            return lib.pyg_block_norm(ctypes.byref(a), *[at(p[n]) for n in ("r", "y", "codes", "steps")], None)
+        for r in base:
+            for o, where in {**base, **inputs}.items():
+                if o != r:
+                    assert rc({**base, r: where + length[o] - 1}) == INVALID, (r, o)
+                    assert rc({**base, r: where - length[r] + 1}) == INVALID, (r, o)
+        need = size(lib.pyg_block_norm_backward_workspace, ctypes.byref(a))[1]
+        grads = ["grad_" + n for n in fields]
+        names = ["grad_r", "grad_y", *grads, "ws"]
+        base = {n: (i + 1) * M for i, n in enumerate(names)}
+        length = {**length, "grad_r": rows, "grad_y": rows, "ws": need, **{"grad_" + n: length[n] for n in fields}}
+
+        def back(p):
+            return lib.pyg_block_norm_backward(ctypes.byref(a), *[at(p[n]) for n in names], need, None)
+        for r in (*grads, "ws"):
+            for o, where in {**base, **inputs}.items():
+                if o != r:
+                    assert back({**base, r: where + length[o] - 1}) == INVALID, (r, o)
+                    assert back({**base, r: where - length[r] + 1}) == INVALID, (r, o)
