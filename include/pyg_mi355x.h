@@ -822,12 +822,12 @@ int pyg_block_norm_backward(const pyg_block_norm_args *a, const void *grad_r, co
  * leaves the block's largest magnitude below 127.5 steps (2^-126 at least); a code is x / step
  * rounded to the nearest integer, ties to even; codes past F are 0. A block that holds an
  * infinity or NaN has steps = 255 and comes back as NaN. Exact up to that one rounding.
- *   x fp32 or bf16; codes 16-byte aligned.
+ *   x fp32 or bf16; codes 16-byte aligned. No array may overlap another.
  * Errors: PYG_ERR_INVALID_ARG, PYG_ERR_UNSUPPORTED (N >= 2^31, F >= 2^24). */
 int pyg_activation_checkpoint(const void *x, int dtype, int64_t N, int64_t F, int8_t *codes, uint8_t *steps,
                               void *stream);
 
-/* x [N, F] = codes * 2^(steps - 127) in dtype (exact in fp32 and in bf16). */
+/* x [N, F] = codes * 2^(steps - 127) in dtype (exact in fp32 and in bf16). Errors: as above. */
 int pyg_checkpoint_restore(const int8_t *codes, const uint8_t *steps, int64_t N, int64_t F, void *x, int dtype,
                            void *stream);
 
@@ -841,8 +841,8 @@ int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int
  * operands enter the matrix cores as three bf16 parts each, which add up to them exactly
  * (magnitudes from 2^-100 on). The products of grad_theta are exact; those of grad_x are off by less than
  * 2^-24 of themselves, to either side (an infinity of G or theta may come out of grad_x as NaN).
- * Deterministic. Errors: PYG_ERR_INVALID_ARG, PYG_ERR_UNSUPPORTED (N >= 2^31, Fi or Fo >=
- * 2^24), PYG_ERR_WORKSPACE. */
+ * Deterministic. Errors: PYG_ERR_INVALID_ARG (also results or a workspace that overlap the inputs or one
+ * another), PYG_ERR_UNSUPPORTED (N >= 2^31, Fi or Fo >= 2^24), PYG_ERR_WORKSPACE. */
 int pyg_dense_transform_backward(const void *grad_out, int dtype, int64_t N, int64_t Fo, const void *theta, int64_t Fi,
                                  const int8_t *codes, const uint8_t *steps, void *grad_x, void *grad_theta, void *ws,
                                  size_t ws_bytes, void *stream);

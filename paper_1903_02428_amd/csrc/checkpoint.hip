@@ -373,6 +373,9 @@ extern "C" int pyg_activation_checkpoint(const void *x, int dtype, int64_t N, in
     if (N >= kMax32 || F >= kMaxF) return PYG_ERR_UNSUPPORTED;
     if (N == 0) return PYG_OK;
     if (!x || !codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16) return PYG_ERR_INVALID_ARG;
+    const Span results[] = {{codes, N * ((F + 31) / 32) * 32}, {steps, N * ((F + 31) / 32)}};
+    const Span inputs[] = {{x, N * F * (dtype == PYG_BF16 ? 2 : 4)}};
+    if (!apart(results, inputs)) return PYG_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int width = static_cast<int>((F + 31) / 32 * 32), f = static_cast<int>(F);
     uint8_t *c = reinterpret_cast<uint8_t *>(codes);
@@ -391,6 +394,9 @@ extern "C" int pyg_checkpoint_restore(const int8_t *codes, const uint8_t *steps,
     if (N >= kMax32 || F >= kMaxF) return PYG_ERR_UNSUPPORTED;
     if (N == 0) return PYG_OK;
     if (!x || !codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16) return PYG_ERR_INVALID_ARG;
+    const Span inputs[] = {{codes, N * ((F + 31) / 32) * 32}, {steps, N * ((F + 31) / 32)}};
+    const Span results[] = {{x, N * F * (dtype == PYG_BF16 ? 2 : 4)}};
+    if (!apart(results, inputs)) return PYG_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int width = static_cast<int>((F + 31) / 32 * 32), f = static_cast<int>(F);
     const uint8_t *c = reinterpret_cast<const uint8_t *>(codes);
@@ -438,6 +444,10 @@ extern "C" int pyg_dense_transform_backward(const void *grad_out, int dtype, int
     if (grad_x && N > 0 && !theta) return PYG_ERR_INVALID_ARG;
     if (grad_theta && N > 0 && (!codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16)) return PYG_ERR_INVALID_ARG;
     if (ws_bytes < need || !ws) return PYG_ERR_WORKSPACE;
+    const int64_t e = dtype == PYG_BF16 ? 2 : 4, blocks = (Fi + 31) / 32;
+    const Span results[] = {{grad_x, N * Fi * e}, {grad_theta, Fi * Fo * e}, {ws, static_cast<int64_t>(need)}};
+    const Span inputs[] = {{grad_out, N * Fo * e}, {theta, Fi * Fo * e}, {codes, N * blocks * 32}, {steps, N * blocks}};
+    if (!apart(results, inputs)) return PYG_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int fi = static_cast<int>(Fi), fo = static_cast<int>(Fo);
     float *part = static_cast<float *>(ws);

@@ -195,3 +195,28 @@ def test_block_norm_overlaps(lib):
                 if o != r:
                     assert back({**base, r: where + length[o] - 1}) == INVALID, (r, o)
                     assert back({**base, r: where - length[r] + 1}) == INVALID, (r, o)
+
+
+def test_checkpoint_and_dense_overlaps(lib):
+    M = 1 << 30
+    for dtype, e in ((0, 4), (1, 2)):
+        length = dict(x=10 * 100 * e, codes=10 * 128, steps=10 * 4)
+        base = {n: (i + 1) * M for i, n in enumerate(length)}
+        for r, o in (("codes", "x"), ("steps", "x"), ("steps", "codes"), ("codes", "steps")):
+            for where in (base[o] + length[o] - 1, base[o] - length[r] + 16):  # codes lie on 16 bytes
+                p = {**base, r: where // 16 * 16}
+                assert lib.pyg_activation_checkpoint(at(p["x"]), dtype, 10, 100, at(p["codes"]), at(p["steps"]), None) == INVALID, (r, o)
+                if o == "x":
+                    assert lib.pyg_checkpoint_restore(at(p["codes"]), at(p["steps"]), 10, 100, at(p["x"]), dtype, None) == INVALID, (r, o)
+        need = size(lib.pyg_dense_transform_backward_workspace, dtype, 1000, 64, 32)[1]
+        length = dict(g=1000 * 32 * e, theta=64 * 32 * e, codes=1000 * 64, steps=1000 * 2, gx=1000 * 64 * e, gt=64 * 32 * e, ws=need)
+        base = {n: (i + 1) * M for i, n in enumerate(length)}
+
+        def rc(p):
+            return lib.pyg_dense_transform_backward(at(p["g"]), dtype, 1000, 32, at(p["theta"]), 64, at(p["codes"]), at(p["steps"]),
+                                                    at(p["gx"]), at(p["gt"]), at(p["ws"]), need, None)
+        for r in ("gx", "gt", "ws"):
+            for o in base:
+                if o != r:
+                    assert rc({**base, r: base[o] + length[o] - 1}) == INVALID, (r, o)
+                    assert rc({**base, r: base[o] - length[r] + 1}) == INVALID, (r, o)
