@@ -33,6 +33,14 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
+// Between LDS accesses of different lanes of one wavefront to the same place. The LDS serves a wavefront in order;
+// this keeps the compiler from another one (no instruction comes of it).
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Adds a 32 x 32 tile of dS^T (rows keys, the lane's column a query) to the wavefront's sums
 // by offset (key - query). The tile is laid down in LDS and read along its 63 diagonals, a lane
 // each, so that no two lanes add to one place: LDS float atomics, a lane at a time, made the
@@ -41,8 +49,10 @@ constexpr int kSkewRow = 40, kSkew = 32 * kSkewRow;  // 40: the two halves' rows
 __device__ __forceinline__ void add_diagonals(const f32x16 &ds, float *own, float *skew, int d0, int reach, int lane) {
     lane = opaque(lane);
     const int m = lane & 31, h = lane >> 5;
+    lanes_meet();  // the last tile's reads
 #pragma unroll
     for (int r = 0; r < 16; ++r) skew[(8 * (r >> 2) + 4 * h + (r & 3)) * kSkewRow + m] = ds[r];
+    lanes_meet();
     const int o = lane - 31;  // the lane's diagonal: key - query of the tile; lane 63 has none
     float t = 0.f;
 #pragma unroll 8
@@ -54,6 +64,7 @@ __device__ __forceinline__ void add_diagonals(const f32x16 &ds, float *own, floa
     const int at = d0 + o;
     const bool mine = lane < 63, low = mine && at < -reach, high = mine && at > reach;
     if (mine && !low && !high) own[at + reach] += t;
+    lanes_meet();  // the ends' sums, of whichever lane
     // the ends stand for all offsets beyond them
     const float below = wave_sum(low ? t : 0.f), above = wave_sum(high ? t : 0.f);
     if (lane == 0) own[0] += below, own[2 * reach] += above;
@@ -259,6 +270,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
     if (mine) {
         below = wave_sum(below), above = wave_sum(above);
+        lanes_meet();
         if (lane == 0) own[0] += below, own[offsets - 1] += above;
         __syncthreads();
         for (int i = threadIdx.x; i < a.buckets; i += NT) {

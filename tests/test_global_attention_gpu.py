@@ -301,3 +301,18 @@ def test_few_queries_infinite_values(pyg, D, dtype):
         assert (out[-1, 2:, 3] == math.inf).all(), out[-1, 2:, 3]
         out[-1, 2:, 3] = ref["out"][0][-1, 2:, 3].to(out.dtype)
         close({"out": out}, ref, f"{D} {dtype} {kn}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("qn,kn,causal", [([20, 31, 5], None, False), ([70, 33], [90, 120], True), ([300, 150], None, False), ([200], [330], True)])
+def test_every_offset_has_its_bucket(pyg, qn, kn, causal, dtype):
+    """A bucket for every offset: each of the table's gradients is the sum of one diagonal, and those beyond the
+    reach the sum of the corners, over several tiles of a wavefront and several wavefronts."""
+    same = kn is None
+    kn = qn if same else kn
+    for reach in (3, 40, 100):
+        q, k, v, grad, _, _ = inputs(13, qn, kn, 3, 1, 24, DT[dtype], 0, 0, causal, pyg)
+        table = torch.randn(2 * reach + 1, 3, generator=torch.Generator().manual_seed(reach)).to(DT[dtype])
+        lut = torch.arange(2 * reach + 1, dtype=torch.int32)
+        got = run(pyg, q, k, v, grad, table, lut, qn, kn, causal, same=same)
+        close(got, attention(q, k, v, qn, kn, table, lut, causal, grad=grad), f"{reach} {dtype}")
