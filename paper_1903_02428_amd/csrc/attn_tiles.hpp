@@ -235,10 +235,13 @@ __device__ __forceinline__ uint32_t lds_offset(const char *p) {
 // every LDS read wait for all such loads; loads_done() waits for them where it is
 // due, ahead of the barrier that hands the tile over.
 __device__ __forceinline__ void load_to_lds(const u32x4 &rsrc, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc)
+    // m0 is the compiler's (it takes no clobber of it) and gets its value back; the load has read it when it was issued
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0\n\ts_nop 0"
+                 : "=&s"(m0)
+                 : "s"(lds), "v"(off), "s"(rsrc)
                  : "memory");
 }
-// (m0 is named nowhere else: these kernels index no register dynamically.)
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // Ahead of a loop with such loads: the wavefront's own loads into registers arrive now, and the
 // compiler knows (vmcnt 0), or the loop's first use of one would wait in every round.
