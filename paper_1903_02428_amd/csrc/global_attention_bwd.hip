@@ -535,74 +535,104 @@ __global__ __launch_bounds__(1024) void k_grad_table(const float *__restrict__ p
 
 constexpr int64_t kMost = (int64_t(1) << 32) - 1;  // threads of a launch
 
+// How a call is cut up. The launches and the workspace go by the same plan.
+struct Plan {
+    bool lone_q, lone_kv;  // workgroups of one wavefront (32 rows) instead of four
+    int q_splits, kv_splits;
+    int64_t q_slots, kv_slots;
+};
+Plan plan_of(const Args &a) {
+    // lone wavefronts for small graphs, as in the forward, and where tiles of 128 are few: one graph of 1,024 nodes
+    // (4 heads of 64, bf16) 111 us against 126, 16 of 512 83 against 100; one of 4,096 (8 heads) 315 against 281.
+    // Ranges of keys are for lone wavefronts too: 2,000 queries of 2 heads of 64 over 100,000 keys (bf16), all
+    // gradients 800 us, 2,570 by workgroups of four that walk all keys.
+    const bool lone = a.Nq <= 128 * a.B || (a.Nq <= 1024 * a.B && a.Nq / 128 * a.H <= 256);
+    Plan p;
+    p.q_splits = q_splits(a);
+    p.lone_q = lone || p.q_splits > 1, p.lone_kv = lone;
+    p.kv_splits = lone ? 1 : kv_splits(a, key_tiles(a));
+    p.q_slots = slots(a.Nq, a.B, p.lone_q ? 32 : 128);
+    p.kv_slots = slots(a.Nk, a.B, p.lone_kv ? 32 : 128);
+    return p;
+}
+
+struct Buffers {
+    float *delta, *table, *kv, *dq;  // table, kv, dq: the shares, or NULL
+    size_t bytes;
+};
+Buffers carve(const Args &a, const Plan &p, bool table, void *ws) {
+    Carver c(ws);
+    Buffers b{};
+    b.delta = c.take<float>(a.Nq * a.H);
+    if (table) b.table = c.take<float>(p.q_slots * p.q_splits * a.H * a.buckets);
+    if (p.kv_splits > 1) b.kv = c.take<float>(2 * p.kv_splits * a.Nk * a.Hkv * a.D);
+    if (p.q_splits > 1) b.dq = c.take<float>(p.q_splits * a.Nq * a.H * a.D);
+    b.bytes = align_up(c.used, 256);
+    return b;
+}
+
 template <typename T, int DP, int WAVES, int BK>
+int launch_q(const BackwardArgs &b, const Plan &p, const Buffers &w, hipStream_t s) {
+    const Args &a = b.f;
+    const size_t pair = 2 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
+    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(p.q_slots * a.H * p.q_splits), 64 * WAVES,
+                                 pair * (WAVES == 1 ? 1 : 2) + bias * (w.table ? 2 + WAVES : 1) +
+                                     (w.table ? WAVES * kSkew * sizeof(float) : 0), s>>>(
+        b, p.q_slots, w.delta, w.table, p.q_splits, w.dq);
+    PYG_LAUNCH_CHECK();
+    return PYG_OK;
+}
+
+template <typename T, int DP, int WAVES, int BK>
+int launch_kv(const BackwardArgs &b, const Plan &p, const Buffers &w, hipStream_t s) {
+    const Args &a = b.f;
+    const size_t pair = 2 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
+    const size_t own = kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0;
+    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(p.kv_slots * a.Hkv * p.kv_splits), 64 * WAVES,
+                                  2 * pair + own + 8 * BK * sizeof(float) + bias, s>>>(b, p.kv_slots, w.delta, p.kv_splits, w.kv);
+    PYG_LAUNCH_CHECK();
+    return PYG_OK;
+}
+
+template <typename T, int DP>
 int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     const Args &a = b.f;
-    const int64_t nq = slots(a.Nq, a.B, 32 * WAVES), nk = slots(a.Nk, a.B, 32 * WAVES);
-    const int splits = WAVES == 1 ? 1 : kv_splits(a, key_tiles(a)), qs = WAVES == 1 ? q_splits(a) : 1;
-    if (nq * a.H * qs * 64 * WAVES > kMost || nk * a.Hkv * splits * 64 * WAVES > kMost) return PYG_ERR_UNSUPPORTED;
-    Carver c(ws);
-    float *delta = c.take<float>(a.Nq * a.H);
-    float *part = c.take<float>(b.grad_table ? nq * qs * a.H * a.buckets : 0);
-    float *kv_part = c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
-    float *dq_part = c.take<float>(qs > 1 ? qs * a.Nq * a.H * a.D : 0);
-    if (!b.grad_table) part = nullptr;
-    const size_t pair = 2 * Tile<T, DP>::template bytes<BK>(), bias = (2 * a.reach + 1) * sizeof(float);
-    k_grad_q<T, DP, WAVES, BK><<<static_cast<unsigned>(nq * a.H * qs), 64 * WAVES,
-                                 pair * (WAVES == 1 ? 1 : 2) + bias * (part ? 2 + WAVES : 1) + (part ? WAVES * kSkew * sizeof(float) : 0), s>>>(
-        b, nq, delta, part, qs, dq_part);
-    PYG_LAUNCH_CHECK();
-    if (qs > 1) {
+    constexpr int BK = DP * sizeof(T) <= 128 ? 64 : 32;  // keys or queries a tile of four wavefronts
+    const Plan p = plan_of(a);
+    if (p.q_slots * a.H * p.q_splits * (p.lone_q ? 64 : 256) > kMost || p.kv_slots * a.Hkv * p.kv_splits * (p.lone_kv ? 64 : 256) > kMost)
+        return PYG_ERR_UNSUPPORTED;
+    const Buffers w = carve(a, p, b.grad_table != nullptr, ws);
+    PYG_TRY((p.lone_q ? launch_q<T, DP, 1, 32>(b, p, w, s) : launch_q<T, DP, 4, BK>(b, p, w, s)));
+    if (w.dq) {
         const int64_t n = a.Nq * a.H * a.D;
-        k_join_q<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(dq_part, n, qs, static_cast<T *>(b.grad_q));
+        k_join_q<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(w.dq, n, p.q_splits, static_cast<T *>(b.grad_q));
         PYG_LAUNCH_CHECK();
     }
-    const size_t own = kValuesInLds<T, DP> ? Tile<T, DP>::template bytes<32 * WAVES>() : 0;
-    k_grad_kv<T, DP, WAVES, BK><<<static_cast<unsigned>(nk * a.Hkv * splits), 64 * WAVES,
-                                  2 * pair + own + 8 * BK * sizeof(float) + bias, s>>>(b, nk, delta, splits, kv_part);
-    PYG_LAUNCH_CHECK();
-    if (splits > 1) {
+    PYG_TRY((p.lone_kv ? launch_kv<T, DP, 1, 32>(b, p, w, s) : launch_kv<T, DP, 4, BK>(b, p, w, s)));
+    if (w.kv) {
         const int64_t n = a.Nk * a.Hkv * a.D;
-        k_join_kv<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(kv_part, n, splits, static_cast<T *>(b.grad_k),
+        k_join_kv<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(w.kv, n, p.kv_splits, static_cast<T *>(b.grad_k),
                                                                   static_cast<T *>(b.grad_v));
         PYG_LAUNCH_CHECK();
     }
-    if (part) {
-        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), 1024, 0, s>>>(part, nq * qs, a.H, a.buckets,
+    if (w.table) {
+        k_grad_table<T><<<dim3(a.H, (a.buckets + 15) / 16), 1024, 0, s>>>(w.table, p.q_slots * p.q_splits, a.H, a.buckets,
                                                                             static_cast<T *>(b.grad_table));
         PYG_LAUNCH_CHECK();
     }
     return PYG_OK;
 }
 
-template <typename T, int DP>
-int by_waves(const BackwardArgs &b, void *ws, hipStream_t s) {
-    // lone wavefronts for small graphs, as in the forward, and where tiles of 128 are few: one graph of 1,024 nodes
-    // (4 heads of 64, bf16) 111 us against 126, 16 of 512 83 against 100; one of 4,096 (8 heads) 315 against 281.
-    const int64_t n = b.f.Nq, g = b.f.B;
-    if (n <= 128 * g || (n <= 1024 * g && n / 128 * b.f.H <= 256)) return launch<T, DP, 1, 32>(b, ws, s);
-    return launch<T, DP, 4, DP * sizeof(T) <= 128 ? 64 : 32>(b, ws, s);
-}
-
 template <typename T>
 int by_width(const BackwardArgs &b, void *ws, hipStream_t s) {
-    if (b.f.D <= 32) return by_waves<T, 32>(b, ws, s);
-    if (b.f.D <= 64) return by_waves<T, 64>(b, ws, s);
-    return by_waves<T, 128>(b, ws, s);
+    if (b.f.D <= 32) return launch<T, 32>(b, ws, s);
+    if (b.f.D <= 64) return launch<T, 64>(b, ws, s);
+    return launch<T, 128>(b, ws, s);
 }
 
 }  // namespace
 
-size_t backward_workspace(const Args &a) {
-    Carver c(nullptr);
-    c.take<float>(a.Nq * a.H);
-    const int qs = q_splits(a);
-    c.take<float>(slots(a.Nq, a.B, 32) * qs * a.H * a.buckets);  // the smallest tiles have the most slots
-    c.take<float>(qs > 1 ? qs * a.Nq * a.H * a.D : 0);
-    const int splits = kv_splits(a, key_tiles(a));
-    c.take<float>(splits > 1 ? 2 * splits * a.Nk * a.Hkv * a.D : 0);
-    return align_up(c.used, 256);
-}
+size_t backward_workspace(const Args &a) { return carve(a, plan_of(a), a.buckets > 0, nullptr).bytes; }
 
 int backward(const BackwardArgs &b, bool bf16, void *ws, hipStream_t s) {
     return bf16 ? by_width<__bf16>(b, ws, s) : by_width<float>(b, ws, s);

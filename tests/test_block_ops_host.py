@@ -220,3 +220,31 @@ def test_checkpoint_and_dense_overlaps(lib):
                 if o != r:
                     assert rc({**base, r: base[o] + length[o] - 1}) == INVALID, (r, o)
                     assert rc({**base, r: base[o] - length[r] + 1}) == INVALID, (r, o)
+
+
+def test_attention_backward_workspace_is_what_is_used(lib):
+    """The workspace holds delta, the table's share of every workgroup (32 rows where wavefronts work alone, 128
+    elsewhere, times the key ranges) and the shares of the one split that the call takes."""
+    def need(**change):
+        a = attention(**change)
+        status, n = size(lib.pyg_global_attention_backward_workspace, ctypes.byref(a))
+        assert status == PYG_OK
+        return n, a
+
+    def total(*parts):
+        return sum(-(-n // 256) * 256 for n in parts)
+    # four wavefronts a workgroup, no heads shared
+    n, a = need(B=1, Nq=9000, Nk=9000, H=16, Hkv=16)
+    assert n == total(9000 * 16 * 4, (9000 // 128 + 2) * 16 * 8 * 4)
+    n, _ = need(B=1, Nq=9000, Nk=9000, H=16, Hkv=16, table=None)
+    assert n == total(9000 * 16 * 4)
+    # and shared by four: the key tiles' 71 * 4 workgroups times the 4 heads of each
+    n, _ = need(B=1, Nq=9000, Nk=9000, H=16, Hkv=4)
+    assert n == total(9000 * 16 * 4, (9000 // 128 + 2) * 16 * 8 * 4, 2 * 4 * 9000 * 4 * 32 * 4)
+    # lone wavefronts: no shares of heads
+    n, _ = need(B=100, Nq=3000, Nk=3000, H=16, Hkv=4)
+    assert n == total(3000 * 16 * 4, (3000 // 32 + 101) * 16 * 8 * 4)
+    # few queries over a long history, also where there are more than 1,024: ranges of keys for dQ
+    for nq, heads, ranges in ((1, 8, 128), (2000, 2, 8)):
+        n, _ = need(B=1, Nq=nq, Nk=100_000, H=heads, Hkv=heads)
+        assert n == total(nq * heads * 4, (nq // 32 + 2) * ranges * heads * 8 * 4, ranges * nq * heads * 32 * 4)

@@ -316,3 +316,12 @@ def test_every_offset_has_its_bucket(pyg, qn, kn, causal, dtype):
         lut = torch.arange(2 * reach + 1, dtype=torch.int32)
         got = run(pyg, q, k, v, grad, table, lut, qn, kn, causal, same=same)
         close(got, attention(q, k, v, qn, kn, table, lut, causal, grad=grad), f"{reach} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("qn,kn,H,Hkv,causal", [([1100], [4500], 2, 1, True), ([1300, 5], [5000, 1200], 1, 1, False)])
+def test_many_queries_over_a_longer_history(pyg, qn, kn, H, Hkv, causal, dtype):
+    """More than 1,024 queries a graph whose keys are still cut into ranges in the backward."""
+    q, k, v, grad, table, lut = inputs(14, qn, kn, H, Hkv, 16, DT[dtype], 8, 64, causal, pyg)
+    got = run(pyg, q, k, v, grad, table, lut, qn, kn, causal)
+    close(got, attention(q, k, v, qn, kn, table, lut, causal, grad=grad), f"{qn} {dtype}")
