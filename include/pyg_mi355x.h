@@ -732,7 +732,9 @@ int pyg_dense_transform(const void *x, int x_dtype, int64_t N, int64_t Fi, const
  *   bucket  int32 [2*reach+1]: the bucket of offset o - reach at place o (offsets
  *           beyond the reach take its ends' buckets). Entries outside [0, buckets) are
  *           read as the nearest one.
- *   zero_rest  non-zero: rows of `out` of no graph get zeros, else they are left as they were. */
+ *   zero_rest  non-zero: rows of `out` of no graph get zeros, else they are left as they were.
+ *   skip    backward: which gradients are not wanted (pyg_attention_skip, or'ed); 0 makes all. */
+typedef enum { PYG_SKIP_GRAD_Q = 1, PYG_SKIP_GRAD_KV = 2, PYG_SKIP_GRAD_TABLE = 4 } pyg_attention_skip;
 typedef struct {
     const int64_t *q_ptr, *k_ptr;
     int64_t B, Nq, Nk, H, Hkv, D;
@@ -744,6 +746,7 @@ typedef struct {
     const int32_t *bucket;
     int64_t buckets, reach;
     int zero_rest;
+    int skip;
 } pyg_attention;
 
 /* Workspace bytes needed by pyg_global_attention (the pointers of *a are not read). */
@@ -770,7 +773,8 @@ int pyg_global_attention_backward_workspace(const pyg_attention *a, size_t *byte
 
 /* Gradients of the above from grad_out [Nq, H, D], the inputs, `out`, `stat` and `rest` (or
  * NULL) of the forward: grad_q [Nq, H, D], grad_k and grad_v [Nk, Hkv, D] (summed over the heads that
- * share a key head in fp32), grad_table [buckets, H] or NULL, all contiguous, in dtype.
+ * share a key head in fp32), grad_table [buckets, H] or NULL, all contiguous, in dtype. Those that
+ * a->skip names are neither made nor written (NULL may stand for them).
  * Rows of no graph get zeros. Deterministic. Errors: as above. */
 int pyg_global_attention_backward(const pyg_attention *a, const void *grad_out, const void *q, const void *k,
                                   const void *v, const void *out, const float *stat, const void *rest, void *grad_q,
@@ -835,7 +839,7 @@ int pyg_checkpoint_restore(const int8_t *codes, const uint8_t *steps, int64_t N,
 int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int64_t Fo, size_t *bytes);
 
 /* Gradients of out = X Theta (pyg_dense_transform) where X was kept in 8 bits:
- *   grad_theta [Fi, Fo] = X^T G with X from codes and steps (NULL with grad_theta NULL);
+ *   grad_theta [Fi, Fo] = X^T G with X from codes and steps (these and ws may be NULL with grad_theta NULL);
  *   grad_x     [N, Fi]  = G Theta^T (theta [Fi, Fo] row-major, or NULL with grad_x NULL);
  * G = grad_out [N, Fo], theta and both results in dtype, fp32 accumulation. fp32
  * operands enter the matrix cores as three bf16 parts each, which add up to them exactly

@@ -72,7 +72,7 @@ class _Attention(ctypes.Structure):
                                        "v_head")] + \
         [("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("causal", ctypes.c_int), ("table", ctypes.c_void_p),
          ("bucket", ctypes.c_void_p), ("buckets", ctypes.c_int64), ("reach", ctypes.c_int64),
-         ("zero_rest", ctypes.c_int)]
+         ("zero_rest", ctypes.c_int), ("skip", ctypes.c_int)]
 
 
 class _BlockNorm(ctypes.Structure):

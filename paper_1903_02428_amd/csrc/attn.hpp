@@ -163,9 +163,13 @@ int forward_few(const Args &a, bool bf16, void *ws, hipStream_t s);
 struct BackwardArgs {
     Args f;  // out: the forward's result
     const void *grad_out;
-    void *grad_q, *grad_k, *grad_v, *grad_table;  // each or NULL (grad_table)
+    void *grad_q, *grad_k, *grad_v, *grad_table;  // NULL: not wanted (grad_k and grad_v together)
 };
-size_t backward_workspace(const Args &a);
+// Which gradients are wanted.
+struct Wanted {
+    bool q, kv, table;
+};
+size_t backward_workspace(const Args &a, const Wanted &w);
 int backward(const BackwardArgs &a, bool bf16, void *ws, hipStream_t s);
 
 }  // namespace attn

@@ -443,7 +443,8 @@ extern "C" int pyg_dense_transform_backward(const void *grad_out, int dtype, int
     if (N > 0 && !grad_out) return PYG_ERR_INVALID_ARG;
     if (grad_x && N > 0 && !theta) return PYG_ERR_INVALID_ARG;
     if (grad_theta && N > 0 && (!codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16)) return PYG_ERR_INVALID_ARG;
-    if (ws_bytes < need || !ws) return PYG_ERR_WORKSPACE;
+    if (!grad_theta) need = 0;  // grad_x works without
+    if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     const int64_t e = dtype == PYG_BF16 ? 2 : 4, blocks = (Fi + 31) / 32;
     const Span results[] = {{grad_x, N * Fi * e}, {grad_theta, Fi * Fo * e}, {ws, static_cast<int64_t>(need)}};
     const Span inputs[] = {{grad_out, N * Fo * e}, {theta, Fi * Fo * e}, {codes, N * blocks * 32}, {steps, N * blocks}};

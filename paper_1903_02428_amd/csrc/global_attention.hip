@@ -265,6 +265,10 @@ int take_inputs(const pyg_attention *c, const void *q, const void *k, const void
     return PYG_OK;
 }
 
+attn::Wanted wanted(const pyg_attention *c) {
+    return {!(c->skip & PYG_SKIP_GRAD_Q), !(c->skip & PYG_SKIP_GRAD_KV), c->table && !(c->skip & PYG_SKIP_GRAD_TABLE)};
+}
+
 // Bytes from the first to the last of N rows of H heads of D features.
 int64_t span(int64_t N, int64_t H, int64_t D, int64_t row, int64_t head, size_t e) {
     return N < 1 ? 0 : static_cast<int64_t>((row * (N - 1) + head * (H - 1) + D) * e);
@@ -325,7 +329,7 @@ extern "C" int pyg_global_attention_backward_workspace(const pyg_attention *c, s
     Args a;
     if (!bytes) return PYG_ERR_INVALID_ARG;
     PYG_TRY(take(c, &a));
-    *bytes = attn::backward_workspace(a);
+    *bytes = attn::backward_workspace(a, wanted(c));
     return PYG_OK;
 }
 
@@ -336,10 +340,14 @@ extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void 
     PYG_TRY(take(c, &b.f));
     PYG_TRY(take_inputs(c, q, k, v, &b.f));
     Args &a = b.f;
-    if (a.Nq > 0 && (!grad_out || !out || !stat || !grad_q)) return PYG_ERR_INVALID_ARG;
-    if (a.Nk > 0 && (!grad_k || !grad_v)) return PYG_ERR_INVALID_ARG;
+    const attn::Wanted want = wanted(c);
+    if (a.Nq > 0 && (!grad_out || !out || !stat || (want.q && !grad_q))) return PYG_ERR_INVALID_ARG;
+    if (a.Nk > 0 && want.kv && (!grad_k || !grad_v)) return PYG_ERR_INVALID_ARG;
     if (grad_table && !c->table) return PYG_ERR_INVALID_ARG;
-    const size_t need = attn::backward_workspace(a);
+    if (!want.q) grad_q = nullptr;
+    if (!want.kv) grad_k = grad_v = nullptr;
+    if (!want.table) grad_table = nullptr;
+    const size_t need = attn::backward_workspace(a, want);
     if (ws_bytes < need || (need && !ws)) return PYG_ERR_WORKSPACE;
     if (rest && c->dtype != PYG_BF16) return PYG_ERR_INVALID_ARG;
     const int64_t e = bytes_of(c), nq = a.Nq * a.H * a.D * e, nk = a.Nk * a.Hkv * a.D * e;
@@ -352,5 +360,6 @@ extern "C" int pyg_global_attention_backward(const pyg_attention *c, const void 
     for (const void *p : {grad_out, out, static_cast<const void *>(grad_q), static_cast<const void *>(grad_k),
                           static_cast<const void *>(grad_v)})
         a.vec_o = a.vec_o && vectors(p, a.D, a.D, a.D, bytes_of(c));
+    if (!want.q && !want.kv && !want.table) return PYG_OK;
     return attn::backward(b, c->dtype == PYG_BF16, ws, static_cast<hipStream_t>(stream));
 }

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     if (pq.tile < 0 || q0 >= pq.last || pq.graph == a.B) {
         if (mine)
             for (int i = threadIdx.x; i < a.buckets; i += NT) mine[i] = 0.f;
-        if (pq.graph == a.B && pq.tile >= 0 && q0 < pq.last) {
+        if (b.grad_q && pq.graph == a.B && pq.tile >= 0 && q0 < pq.last) {
             const int64_t e = q0 + BM < pq.last ? q0 + BM : pq.last;
             if (splits > 1) zero_rows(dq_part, q0, e, a.H, head, a.D);
             else zero_rows(static_cast<T *>(b.grad_q), q0, e, a.H, head, a.D);
@@ -133,6 +133,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         from = sp * share;
         end = end < from + share ? end : from + share;
     }
+    if (!b.grad_q && !mine) end = from;  // delta alone is wanted
     const Stage<T, DP, BK, NT> sk(a.k_row, a.D, a.vec_k), sv(a.v_row, a.D, a.vec_v);
     auto fetch = [&](int64_t j0, int half) {
         if (j0 >= end) return;
@@ -266,8 +267,10 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
             step(lds + 2 * kTile, lds + 3 * kTile, j0 + BK);
         }
     }
-    if (splits > 1) store_rows<float, DP>(dq_part, row, there, a.H, head, a.D, a.D % 4 == 0, acc, a.scale, lane);
-    else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
+    if (b.grad_q) {
+        if (splits > 1) store_rows<float, DP>(dq_part, row, there, a.H, head, a.D, a.D % 4 == 0, acc, a.scale, lane);
+        else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
+    }
     if (mine) {
         below = wave_sum(below), above = wave_sum(above);
         lanes_meet();
@@ -541,14 +544,14 @@ struct Plan {
     int q_splits, kv_splits;
     int64_t q_slots, kv_slots;
 };
-Plan plan_of(const Args &a) {
+Plan plan_of(const Args &a, const Wanted &want) {
     // lone wavefronts for small graphs, as in the forward, and where tiles of 128 are few: one graph of 1,024 nodes
     // (4 heads of 64, bf16) 111 us against 126, 16 of 512 83 against 100; one of 4,096 (8 heads) 315 against 281.
     // Ranges of keys are for lone wavefronts too: 2,000 queries of 2 heads of 64 over 100,000 keys (bf16), all
     // gradients 800 us, 2,570 by workgroups of four that walk all keys.
     const bool lone = a.Nq <= 128 * a.B || (a.Nq <= 1024 * a.B && a.Nq / 128 * a.H <= 256);
     Plan p;
-    p.q_splits = q_splits(a);
+    p.q_splits = want.q || want.table ? q_splits(a) : 1;
     p.lone_q = lone || p.q_splits > 1, p.lone_kv = lone;
     p.kv_splits = lone ? 1 : kv_splits(a, key_tiles(a));
     p.q_slots = slots(a.Nq, a.B, p.lone_q ? 32 : 128);
@@ -560,13 +563,13 @@ struct Buffers {
     float *delta, *table, *kv, *dq;  // table, kv, dq: the shares, or NULL
     size_t bytes;
 };
-Buffers carve(const Args &a, const Plan &p, bool table, void *ws) {
+Buffers carve(const Args &a, const Plan &p, const Wanted &want, void *ws) {
     Carver c(ws);
     Buffers b{};
     b.delta = c.take<float>(a.Nq * a.H);
-    if (table) b.table = c.take<float>(p.q_slots * p.q_splits * a.H * a.buckets);
-    if (p.kv_splits > 1) b.kv = c.take<float>(2 * p.kv_splits * a.Nk * a.Hkv * a.D);
-    if (p.q_splits > 1) b.dq = c.take<float>(p.q_splits * a.Nq * a.H * a.D);
+    if (want.table) b.table = c.take<float>(p.q_slots * p.q_splits * a.H * a.buckets);
+    if (want.kv && p.kv_splits > 1) b.kv = c.take<float>(2 * p.kv_splits * a.Nk * a.Hkv * a.D);
+    if (want.q && p.q_splits > 1) b.dq = c.take<float>(p.q_splits * a.Nq * a.H * a.D);
     b.bytes = align_up(c.used, 256);
     return b;
 }
@@ -598,17 +601,18 @@ template <typename T, int DP>
 int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     const Args &a = b.f;
     constexpr int BK = DP * sizeof(T) <= 128 ? 64 : 32;  // keys or queries a tile of four wavefronts
-    const Plan p = plan_of(a);
+    const Wanted want{b.grad_q != nullptr, b.grad_k != nullptr, b.grad_table != nullptr};
+    const Plan p = plan_of(a, want);
     if (p.q_slots * a.H * p.q_splits * (p.lone_q ? 64 : 256) > kMost || p.kv_slots * a.Hkv * p.kv_splits * (p.lone_kv ? 64 : 256) > kMost)
         return PYG_ERR_UNSUPPORTED;
-    const Buffers w = carve(a, p, b.grad_table != nullptr, ws);
+    const Buffers w = carve(a, p, want, ws);
     PYG_TRY((p.lone_q ? launch_q<T, DP, 1, 32>(b, p, w, s) : launch_q<T, DP, 4, BK>(b, p, w, s)));
     if (w.dq) {
         const int64_t n = a.Nq * a.H * a.D;
         k_join_q<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(w.dq, n, p.q_splits, static_cast<T *>(b.grad_q));
         PYG_LAUNCH_CHECK();
     }
-    PYG_TRY((p.lone_kv ? launch_kv<T, DP, 1, 32>(b, p, w, s) : launch_kv<T, DP, 4, BK>(b, p, w, s)));
+    if (want.kv) PYG_TRY((p.lone_kv ? launch_kv<T, DP, 1, 32>(b, p, w, s) : launch_kv<T, DP, 4, BK>(b, p, w, s)));
     if (w.kv) {
         const int64_t n = a.Nk * a.Hkv * a.D;
         k_join_kv<T><<<grid_for(n, kBlock, 8192), kBlock, 0, s>>>(w.kv, n, p.kv_splits, static_cast<T *>(b.grad_k),
@@ -632,7 +636,7 @@ int by_width(const BackwardArgs &b, void *ws, hipStream_t s) {
 
 }  // namespace
 
-size_t backward_workspace(const Args &a) { return carve(a, plan_of(a), a.buckets > 0, nullptr).bytes; }
+size_t backward_workspace(const Args &a, const Wanted &want) { return carve(a, plan_of(a, want), want, nullptr).bytes; }
 
 int backward(const BackwardArgs &b, bool bf16, void *ws, hipStream_t s) {
     return bf16 ? by_width<__bf16>(b, ws, s) : by_width<float>(b, ws, s);

@@ -75,7 +75,7 @@ def _heads(name, t, dtype=None, device=None):
     return t
 
 
-def _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, zero_rest) -> _Attention:
+def _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, zero_rest, skip=0) -> _Attention:
     _heads("q", q)
     _heads("k", k, q.dtype)
     _heads("v", v, q.dtype)
@@ -107,7 +107,7 @@ def _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, zero_rest) ->
     return _Attention(ptr.data_ptr(), k_ptr.data_ptr(), ptr.shape[0] - 1, Nq, Nk, H, Hkv, D, q.stride(0), q.stride(1),
                       k.stride(0), k.stride(1), v.stride(0), v.stride(1), DTYPE[q.dtype], scale, int(bool(causal)),
                       _ptr(table), _ptr(buckets), 0 if table is None else table.shape[0],
-                      0 if table is None else buckets.shape[0] // 2, int(zero_rest))
+                      0 if table is None else buckets.shape[0] // 2, int(zero_rest), skip)
 
 
 def _bytes(fn, c) -> int:
@@ -175,11 +175,14 @@ def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
                               k_ptr: torch.Tensor | None = None, table: torch.Tensor | None = None,
                               buckets: torch.Tensor | None = None, causal: bool = False, scale: float | None = None,
                               need_grad_table: bool = True, rest: torch.Tensor | None = None,
-                              workspace: torch.Tensor | None = None):
-    """Gradients of global_attention: (grad_q, grad_k, grad_v, grad_table or
-    None), from its result `out`, the `stat` and, if it was asked for, the `rest` it filled."""
+                              workspace: torch.Tensor | None = None, need_grad_q: bool = True,
+                              need_grad_kv: bool = True):
+    """Gradients of global_attention: (grad_q, grad_k, grad_v, grad_table), None for those
+    that are not needed, from its result `out`, the `stat` and, if it was asked for, the `rest` it filled."""
     lib = library()
-    c = _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, True)
+    need_grad_table = need_grad_table and table is not None
+    c = _attention(q, k, v, ptr, k_ptr, table, buckets, causal, scale, True,
+                   (not need_grad_q) + 2 * (not need_grad_kv) + 4 * (not need_grad_table))
     dev = q.device
     for name, t in (("grad_out", grad_out), ("out", out)):
         _need_cuda(name, t, q.dtype, 3)
@@ -190,8 +193,9 @@ def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
         raise ValueError("stat must be [rows, heads, 2]")
     _rest(rest, q)
     _same_device(dev, grad_out=grad_out, out=out, stat=stat, rest=rest, workspace=workspace)
-    gq, gk, gv = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
-    gt = torch.empty_like(table) if table is not None and need_grad_table else None
+    gq, gk, gv = (torch.empty(t.shape, dtype=t.dtype, device=dev) if need else None
+                  for t, need in ((q, need_grad_q), (k, need_grad_kv), (v, need_grad_kv)))
+    gt = torch.empty_like(table) if need_grad_table else None
     with _on(dev):
         nbytes = _bytes(lib.pyg_global_attention_backward_workspace, c)
         if workspace is None or workspace.numel() < nbytes:
@@ -227,8 +231,10 @@ class GlobalAttention(torch.autograd.Function):
         q, k, v, table, out, stat, rest, ptr, k_ptr, buckets = ctx.saved_tensors
         qc, kc, vc = (_adjacent(t.detach()) for t in (q, k, v))
         tc = None if table is None else table.detach().contiguous()
+        need = ctx.needs_input_grad
         grads = global_attention_backward(grad_out.to(q.dtype).contiguous(), qc, kc, vc, out.contiguous(), stat, ptr, k_ptr,
-                                          tc, buckets, ctx.causal, ctx.scale, need_grad_table=ctx.needs_input_grad[3], rest=rest)
+                                          tc, buckets, ctx.causal, ctx.scale, need_grad_table=need[3], rest=rest,
+                                          need_grad_q=need[0], need_grad_kv=need[1] or need[2])
         return tuple(g if need else None for g, need in zip(grads, ctx.needs_input_grad)) + (None,) * 5
 
 
@@ -336,12 +342,13 @@ def dense_transform_backward(grad_out: torch.Tensor, theta: torch.Tensor, kept: 
     gx = torch.empty((N, Fi), dtype=theta.dtype, device=dev) if need_grad_x else None
     gt = torch.empty_like(theta) if need_grad_theta else None
     with _on(dev):
-        nbytes = _size(lib.pyg_dense_transform_backward_workspace, DTYPE[theta.dtype], N, Fi, Fo)
-        if workspace is None or workspace.numel() < nbytes:
+        nbytes = _size(lib.pyg_dense_transform_backward_workspace, DTYPE[theta.dtype], N, Fi, Fo) if need_grad_theta else 0
+        if nbytes and (workspace is None or workspace.numel() < nbytes):
             workspace = _workspace(nbytes, dev)
         _check(lib.pyg_dense_transform_backward(_ptr(grad_out), DTYPE[theta.dtype], N, Fo, _ptr(theta), Fi,
-                                                _ptr(kept.codes) if kept else None, _ptr(kept.steps) if kept else None, _ptr(gx), _ptr(gt), _ptr(workspace),
-                                                workspace.numel(), _stream(dev)), "pyg_dense_transform_backward")
+                                                _ptr(kept.codes) if kept else None, _ptr(kept.steps) if kept else None,
+                                                _ptr(gx), _ptr(gt), _ptr(workspace) if nbytes else None, nbytes,
+                                                _stream(dev)), "pyg_dense_transform_backward")
     return gx, gt
 
 

@@ -248,3 +248,27 @@ def test_attention_backward_workspace_is_what_is_used(lib):
     for nq, heads, ranges in ((1, 8, 128), (2000, 2, 8)):
         n, _ = need(B=1, Nq=nq, Nk=100_000, H=heads, Hkv=heads)
         assert n == total(nq * heads * 4, (nq // 32 + 2) * ranges * heads * 8 * 4, ranges * nq * heads * 32 * 4)
+
+
+def test_gradients_that_are_not_wanted(lib):
+    """Neither arrays nor workspace for them."""
+    def need(**change):
+        status, n = size(lib.pyg_global_attention_backward_workspace, ctypes.byref(attention(B=1, Nq=9000, Nk=9000, H=16, Hkv=4, **change)))
+        assert status == PYG_OK
+        return n
+    delta = 9000 * 16 * 4
+    assert need(skip=4) == need() - (9000 // 128 + 2) * 16 * 8 * 4 and need(skip=2) == need() - 2 * 4 * 9000 * 4 * 32 * 4
+    assert need(skip=7) == need(skip=6) == delta
+    a = attention(B=1, Nq=1, Nk=100_000, H=8, Hkv=8)
+    b = attention(B=1, Nq=1, Nk=100_000, H=8, Hkv=8, skip=5)
+    assert size(lib.pyg_global_attention_backward_workspace, ctypes.byref(b))[1] == 256 < size(lib.pyg_global_attention_backward_workspace, ctypes.byref(a))[1]
+
+    def back(a, gq=D_, gk=B_, gv=C_, gt=A, ws=at(5 << 30)):
+        return lib.pyg_global_attention_backward(ctypes.byref(a), at(6 << 30), at(7 << 30), at(8 << 30), at(9 << 30), at(10 << 30),
+                                                 at(11 << 30), None, gq, gk, gv, gt, ws, 1 << 30, None)
+    assert back(attention(skip=7), None, None, None, None) == PYG_OK  # nothing to do
+    assert back(attention(skip=1), gk=None) == INVALID and back(attention(skip=2), gq=None) == INVALID
+    # the dense transform's: N = 0 leaves nothing to launch
+    dense = lib.pyg_dense_transform_backward
+    assert dense(None, 0, 0, 32, B_, 64, None, None, D_, None, None, 0, None) == PYG_OK
+    assert dense(None, 0, 0, 32, B_, 64, None, None, D_, A, None, 0, None) == WORKSPACE

@@ -325,3 +325,26 @@ def test_many_queries_over_a_longer_history(pyg, qn, kn, H, Hkv, causal, dtype):
     q, k, v, grad, table, lut = inputs(14, qn, kn, H, Hkv, 16, DT[dtype], 8, 64, causal, pyg)
     got = run(pyg, q, k, v, grad, table, lut, qn, kn, causal)
     close(got, attention(q, k, v, qn, kn, table, lut, causal, grad=grad), f"{qn} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("qn,kn", [([1, 2], [2500, 2000]), ([20, 45], [50, 90]), ([150, 3], [200, 130])])
+def test_gradients_that_are_not_wanted(pyg, qn, kn, dtype):
+    """Each set of wanted gradients is what the whole call gives of it, to the bit, with rows of no graph behind."""
+    q, k, v, grad, table, lut = (t.cuda() for t in inputs(15, qn, kn, 4, 2, 32, DT[dtype], 8, 16, True, pyg, extra=3))
+    stat = torch.empty((*q.shape[:2], 2), device="cuda")
+    args = (ptr_of(qn), ptr_of(kn), table, lut, True)
+    out = pyg.global_attention(q, k, v, *args, stat=stat)
+    whole = pyg.global_attention_backward(grad, q, k, v, out, stat, *args)
+    for wanted in range(8):
+        a, b, c = bool(wanted & 1), bool(wanted & 2), bool(wanted & 4)
+        got = pyg.global_attention_backward(grad, q, k, v, out, stat, *args, need_grad_q=a, need_grad_kv=b, need_grad_table=c)
+        for x, y, need in zip(got, whole, (a, b, b, c)):
+            assert torch.equal(x, y) if need else x is None
+    for i in range(4):  # and through autograd
+        leaves = [t.clone().requires_grad_(i == j) for j, t in enumerate((q, k, v, table))]
+        out = pyg.GlobalAttention.apply(*leaves, args[0], args[1], lut, True)
+        got, = torch.autograd.grad(out, [leaves[i]], grad)
+        full = [t.clone().requires_grad_(True) for t in (q, k, v, table)]
+        out = pyg.GlobalAttention.apply(*full, args[0], args[1], lut, True)
+        assert torch.equal(got, torch.autograd.grad(out, full, grad)[i])
