@@ -846,7 +846,7 @@ int pyg_dense_transform_backward_workspace(int dtype, int64_t N, int64_t Fi, int
  * (magnitudes from 2^-100 on). The products of grad_theta are exact; those of grad_x are off by less than
  * 2^-24 of themselves, to either side (an infinity of G or theta may come out of grad_x as NaN).
  * Deterministic. Errors: PYG_ERR_INVALID_ARG (also results or a workspace that overlap the inputs or one
- * another), PYG_ERR_UNSUPPORTED (N >= 2^31, Fi or Fo >= 2^24), PYG_ERR_WORKSPACE. */
+ * another), PYG_ERR_UNSUPPORTED (N >= 2^31, Fi or Fo >= 2^24, a grid of 2^32 threads), PYG_ERR_WORKSPACE. */
 int pyg_dense_transform_backward(const void *grad_out, int dtype, int64_t N, int64_t Fo, const void *theta, int64_t Fi,
                                  const int8_t *codes, const uint8_t *steps, void *grad_x, void *grad_theta, void *ws,
                                  size_t ws_bytes, void *stream);

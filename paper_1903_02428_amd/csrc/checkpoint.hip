@@ -319,19 +319,22 @@ __global__ __launch_bounds__(kBlock) void k_input_grad(const T *__restrict__ g, 
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_join_theta(const float *__restrict__ part, int64_t n, int splits,
                                                        T *__restrict__ out) {
-    // 32 values a workgroup, 8 threads a value
+    // 32 values at a time, 8 threads a value
     __shared__ float lds[8][32];
     const int i = threadIdx.x & 31, r = threadIdx.x >> 5;
-    const int64_t at = (int64_t)blockIdx.x * 32 + i;
-    float v = 0.f;
-    if (at < n)
+    for (int64_t first = (int64_t)blockIdx.x * 32; first < n; first += (int64_t)gridDim.x * 32) {
+        const int64_t at = first + i;
+        float v = 0.f;
+        if (at < n)
 #pragma unroll 8
-        for (int s = r; s < splits; s += 8) v += part[(int64_t)s * n + at];
-    lds[r][i] = v;
-    __syncthreads();
-    if (r == 0 && at < n) {
-        for (int k = 1; k < 8; ++k) v += lds[k][i];
-        out[at] = T(v);
+            for (int s = r; s < splits; s += 8) v += part[(int64_t)s * n + at];
+        lds[r][i] = v;
+        __syncthreads();
+        if (r == 0 && at < n) {
+            for (int k = 1; k < 8; ++k) v += lds[k][i];
+            out[at] = T(v);
+        }
+        __syncthreads();
     }
 }
 
@@ -339,8 +342,9 @@ constexpr int64_t kMax32 = int64_t(1) << 31, kMaxF = int64_t(1) << 24;
 
 // Row ranges of dTheta: two workgroups a CU, 128 rows or more each (19,717 rows, 500 to 64 features, bf16:
 // 256 rows 20 us, 128 18).
+int64_t theta_tiles(int64_t Fi, int64_t Fo) { return ((Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO); }
 int splits_of(int64_t N, int64_t Fi, int64_t Fo) {
-    const int64_t tiles = ((Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO);
+    const int64_t tiles = theta_tiles(Fi, Fo);
     int64_t s = 512 / tiles, most = N / 128;
     s = s < most ? s : most;
     return static_cast<int>(s < 1 ? 1 : s);
@@ -352,12 +356,11 @@ template <typename T>
 int theta_grad(const T *g, int64_t N, int Fo, int Fi, const int8_t *codes, const uint8_t *steps, T *out, float *part,
                hipStream_t s) {
     const int splits = splits_of(N, Fi, Fo), blocks = (Fi + 31) / 32;
-    const int64_t tiles = ((int64_t)(Fi + kTileI - 1) / kTileI) * ((Fo + kTileO - 1) / kTileO), n = (int64_t)Fi * Fo;
-    if (tiles * splits * kBlock >= (int64_t(1) << 32) || n / 32 * kBlock >= (int64_t(1) << 32)) return PYG_ERR_UNSUPPORTED;
+    const int64_t tiles = theta_tiles(Fi, Fo), n = (int64_t)Fi * Fo;
     k_theta_grad<T, sizeof(T) == 2 ? 1 : 3><<<static_cast<unsigned>(tiles * splits), kBlock, 0, s>>>(
         reinterpret_cast<const uint8_t *>(codes), steps, g, N, Fi, Fo, blocks, splits, part);
     PYG_LAUNCH_CHECK();
-    k_join_theta<T><<<static_cast<unsigned>((n + 31) / 32), kBlock, 0, s>>>(part, n, splits, out);
+    k_join_theta<T><<<grid_for(n, 32), kBlock, 0, s>>>(part, n, splits, out);
     PYG_LAUNCH_CHECK();
     return PYG_OK;
 }
@@ -421,9 +424,7 @@ int check_dense(int dtype, int64_t N, int64_t Fi, int64_t Fo, size_t *bytes) {
 template <typename T>
 int input_grad(const T *g, const T *theta, int64_t N, int Fi, int Fo, T *out, hipStream_t s) {
     const int tiles_i = (Fi + 127) / 128;
-    const int64_t grid = (N + 127) / 128 * tiles_i;
-    if (grid * kBlock >= (int64_t(1) << 32)) return PYG_ERR_UNSUPPORTED;
-    k_input_grad<T, sizeof(T) == 2 ? 1 : 3><<<static_cast<unsigned>(grid), kBlock, 0, s>>>(
+    k_input_grad<T, sizeof(T) == 2 ? 1 : 3><<<static_cast<unsigned>((N + 127) / 128 * tiles_i), kBlock, 0, s>>>(
         g, theta, N, Fi, Fo, tiles_i, Fi % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0, out);
     PYG_LAUNCH_CHECK();
     return PYG_OK;
@@ -440,6 +441,10 @@ extern "C" int pyg_dense_transform_backward(const void *grad_out, int dtype, int
                                             void *grad_theta, void *ws, size_t ws_bytes, void *stream) {
     size_t need = 0;
     PYG_TRY(check_dense(dtype, N, Fi, Fo, &need));
+    // before anything is launched: either result's grid
+    constexpr int64_t most = (int64_t(1) << 32) / kBlock;
+    if ((grad_x && (N + 127) / 128 * ((Fi + 127) / 128) >= most) || (grad_theta && theta_tiles(Fi, Fo) * splits_of(N, Fi, Fo) >= most))
+        return PYG_ERR_UNSUPPORTED;
     if (N > 0 && !grad_out) return PYG_ERR_INVALID_ARG;
     if (grad_x && N > 0 && !theta) return PYG_ERR_INVALID_ARG;
     if (grad_theta && N > 0 && (!codes || !steps || reinterpret_cast<uintptr_t>(codes) % 16)) return PYG_ERR_INVALID_ARG;

@@ -272,3 +272,11 @@ def test_gradients_that_are_not_wanted(lib):
     dense = lib.pyg_dense_transform_backward
     assert dense(None, 0, 0, 32, B_, 64, None, None, D_, None, None, 0, None) == PYG_OK
     assert dense(None, 0, 0, 32, B_, 64, None, None, D_, A, None, 0, None) == WORKSPACE
+
+
+def test_dense_sizes_are_refused_before_anything_is_launched(lib):
+    """A grid that one of the two results cannot have, also where the other could be made first."""
+    def rc(N, Fi, Fo, gx, gt):
+        return lib.pyg_dense_transform_backward(A, 0, N, Fo, B_, Fi, C_, C_, gx, gt, D_, 1 << 62, None)
+    assert rc(1, 1 << 23, 1 << 23, D_, A) == UNSUPPORTED and rc(1, 1 << 23, 1 << 23, None, A) == UNSUPPORTED
+    assert rc((1 << 31) - 1, 1 << 23, 1, D_, None) == UNSUPPORTED
