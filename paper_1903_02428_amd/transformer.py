@@ -207,7 +207,9 @@ def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
 
 
 def _adjacent(t):
-    return t if t.dim() != 3 or t.shape[2] <= 1 or t.stride(2) == 1 and 0 not in t.stride() else t.contiguous()
+    """Features adjacent and no row or head standing for several, by a copy where it takes one."""
+    fits = t.dim() != 3 or (t.shape[2] <= 1 or t.stride(2) == 1) and 0 not in t.stride()
+    return t if fits else t.contiguous()
 
 
 class GlobalAttention(torch.autograd.Function):

@@ -348,3 +348,21 @@ def test_gradients_that_are_not_wanted(pyg, qn, kn, dtype):
         full = [t.clone().requires_grad_(True) for t in (q, k, v, table)]
         out = pyg.GlobalAttention.apply(*full, args[0], args[1], lut, True)
         assert torch.equal(got, torch.autograd.grad(out, full, grad)[i])
+
+
+@pytest.mark.parametrize("D", [1, 8])
+def test_broadcast_inputs(pyg, D):
+    """One row or head that stands for all of them: the gradient of the small tensor is the sum."""
+    n, H = [9, 40], 4
+    g = torch.Generator().manual_seed(16)
+    grad = torch.randn(sum(n), H, D, generator=g)
+    small = [torch.randn(sum(n), 1, D, generator=g), torch.randn(1, H, D, generator=g), torch.randn(sum(n), 1, D, generator=g)]
+    whole = [t.expand(sum(n), H, D) for t in small]
+    ref = attention(*whole, n, n, grad=grad)
+    leaves = [t.cuda().requires_grad_(True) for t in small]
+    out = pyg.GlobalAttention.apply(*[t.expand(sum(n), H, D) for t in leaves], None, ptr_of(n))
+    grads = torch.autograd.grad(out, leaves, grad.cuda())
+    close({"out": out}, ref, "out")
+    for name, got, dim in zip(("grad_q", "grad_k", "grad_v"), grads, (1, 0, 1)):
+        val, bound = (t.sum(dim, keepdim=True) for t in ref[name])  # and the sum in fp32 of so many terms
+        close({name: got}, {name: (val, bound + sum(n) * 2.0 ** -24 * ref[name][0].abs().sum(dim, keepdim=True))}, "broadcast")
