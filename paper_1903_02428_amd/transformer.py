@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 from dataclasses import dataclass
 
@@ -33,6 +34,33 @@ def _written(*tensors):
     for t in tensors:
         if t is not None and not t.is_inference():
             torch.autograd.graph.increment_version(t)
+
+
+class _Gradient(torch.autograd.Function):
+    """A gradient that was asked for with create_graph, tied to what it depends on: differentiating
+    it raises."""
+
+    @staticmethod
+    def forward(ctx, gradient, *depends):
+        return gradient.view_as(gradient)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("this operator can be differentiated once: its gradients have none themselves")
+
+
+def _once(backward):
+    """For a backward that calls kernels, which autograd does not see: without this its results would
+    count as constants in a second differentiation, and terms be left out silently."""
+    @functools.wraps(backward)
+    def wrapper(ctx, *grads):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        depends = [t for t in (*grads, *ctx.saved_tensors) if t is not None and t.requires_grad]
+        return tuple(None if t is None else _Gradient.apply(t, *depends) for t in out)
+    return wrapper
 
 
 def relative_buckets(num_buckets: int = 32, max_distance: int = 128, bidirectional: bool = True,
@@ -229,6 +257,7 @@ class GlobalAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_once
     def backward(ctx, grad_out):
         q, k, v, table, out, stat, rest, ptr, k_ptr, buckets = ctx.saved_tensors
         qc, kc, vc = (_adjacent(t.detach()) for t in (q, k, v))
@@ -375,6 +404,7 @@ class DenseTransform(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_once
     def backward(ctx, grad_out):
         theta, *held = ctx.saved_tensors
         g, t = grad_out.to(theta.dtype).contiguous(), theta.detach().contiguous()
@@ -499,6 +529,7 @@ class BlockNorm(torch.autograd.Function):
         return r, y, kept
 
     @staticmethod
+    @_once
     def backward(ctx, grad_r, grad_y, _):
         tensors = ctx.saved_tensors
         if grad_r is None and grad_y is None:

@@ -140,3 +140,24 @@ def test_captured_forward(pyg):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(r, want[0]) and torch.equal(y2, want[1])
+
+
+def test_second_derivatives_are_refused(pyg):
+    """Gradients of the gradients do not exist: asked for, they raise instead of leaving terms out."""
+    x = torch.randn(12, 64, device="cuda", requires_grad=True)
+    ptr = torch.tensor([0, 12], device="cuda")
+    w = torch.randn(64, 64, device="cuda", requires_grad=True)
+    one = torch.ones(64, device="cuda")
+    calls = ((x, lambda: pyg.GlobalAttention.apply(*[x.view(12, 4, 16)] * 3, None, ptr)), (w, lambda: pyg.DenseTransform.apply(x, w)),
+             (x, lambda: pyg.BlockNorm.apply(x, x, None, None, None, None, one)[1]))
+    for by, call in calls:
+        out = call()
+        go = torch.randn_like(out)
+        g, = torch.autograd.grad(out, [x], go, create_graph=True)
+        assert torch.equal(g, torch.autograd.grad(call(), [x], go)[0])
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            torch.autograd.grad(g.square().sum() + by.square().sum(), [by])
+        go.requires_grad_(True)
+        g, = torch.autograd.grad(call(), [x], go, create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            torch.autograd.grad(g.square().sum(), [go])
