@@ -399,7 +399,10 @@ class DenseTransform(torch.autograd.Function):
                 raise ValueError("kept must be the checkpoint of x")
             ctx.F = kept.F
         ctx.shape = tuple(x.shape)
-        out = dense_transform(xc, tc, x.dtype)
+        _need_cuda("x", xc, None, 2)
+        _same_device(x.device, theta=tc)
+        with _on(x.device):
+            out = dense_transform(xc, tc, x.dtype)
         ctx.save_for_backward(theta, *((kept.codes, kept.steps) if ctx.F else ()))
         return out
 

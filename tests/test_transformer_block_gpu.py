@@ -161,3 +161,32 @@ def test_second_derivatives_are_refused(pyg):
         g, = torch.autograd.grad(call(), [x], go, create_graph=True)
         with pytest.raises(RuntimeError, match="differentiated once"):
             torch.autograd.grad(g.square().sum(), [go])
+
+
+def test_calls_go_to_the_tensors_device(pyg, monkeypatch):
+    """Every kernel is launched with the tensors' device as the current one (a second device stood in for by
+    watching the guard that each call takes)."""
+    import contextlib
+
+    from paper_1903_02428_amd import transformer
+    depth, seen = [0], []
+
+    @contextlib.contextmanager
+    def guard(device):
+        assert device == torch.device("cuda", 0)
+        depth[0] += 1
+        yield
+        depth[0] -= 1
+    monkeypatch.setattr(transformer, "_on", guard)
+    stream, whole = transformer._stream, transformer.dense_transform
+    monkeypatch.setattr(transformer, "_stream", lambda d: (seen.append(depth[0]), stream(d))[1])
+    monkeypatch.setattr(transformer, "dense_transform", lambda *a: (seen.append(depth[0]), whole(*a))[1])
+    p, gr, gy = params()
+    ptr = torch.tensor(np.concatenate([[0], np.cumsum(LENGTHS)]), dtype=torch.int64, device="cuda")
+    run(pyg, p, gr, gy, ptr, pyg.relative_buckets(BUCKETS, 16))
+    kept = pyg.activation_checkpoint(gr.cuda())
+    pyg.checkpoint_restore(kept)
+    # two norms, three transforms (two of them from a checkpoint), an attention, all forward and backward, and the two above
+    assert len(seen) == 2 * 2 + (3 + 1 + 3) + 2 + 2 and all(seen)
+    with pytest.raises(ValueError):
+        pyg.DenseTransform.apply(gr, p["w_gate"])
