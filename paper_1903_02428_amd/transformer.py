@@ -36,6 +36,17 @@ def _written(*tensors):
             torch.autograd.graph.increment_version(t)
 
 
+def _room(workspace, nbytes: int, device):
+    """The caller's workspace where it is large enough, else one made here."""
+    if workspace is not None:
+        _need_cuda("workspace", workspace)  # adjacent bytes: as many as its elements have
+        if not _aligned16(workspace):
+            raise ValueError("workspace must be 16-byte aligned")
+        if workspace.numel() * workspace.element_size() >= nbytes:
+            return workspace
+    return _workspace(nbytes, device)
+
+
 class _Gradient(torch.autograd.Function):
     """A gradient that was asked for with create_graph, tied to what it depends on: differentiating
     it raises."""
@@ -183,8 +194,7 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
     _same_device(dev, out=out, stat=stat, rest=rest, workspace=workspace)
     with _on(dev):
         nbytes = _bytes(lib.pyg_global_attention_workspace, c)
-        if nbytes and (workspace is None or workspace.numel() < nbytes):
-            workspace = _workspace(nbytes, dev)
+        workspace = _room(workspace, nbytes, dev) if nbytes else None
         _check(lib.pyg_global_attention(ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(stat),
                                         _ptr(rest), _ptr(workspace), nbytes, _stream(dev)), "pyg_global_attention")
     _written(given, stat, rest)
@@ -226,11 +236,10 @@ def global_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     gt = torch.empty_like(table) if need_grad_table else None
     with _on(dev):
         nbytes = _bytes(lib.pyg_global_attention_backward_workspace, c)
-        if workspace is None or workspace.numel() < nbytes:
-            workspace = _workspace(nbytes, dev)
+        workspace = _room(workspace, nbytes, dev)
         _check(lib.pyg_global_attention_backward(ctypes.byref(c), _ptr(grad_out), _ptr(q), _ptr(k), _ptr(v), _ptr(out),
                                                  _ptr(stat), _ptr(rest), _ptr(gq), _ptr(gk), _ptr(gv), _ptr(gt), _ptr(workspace),
-                                                 workspace.numel(), _stream(dev)), "pyg_global_attention_backward")
+                                                 nbytes, _stream(dev)), "pyg_global_attention_backward")
     return gq, gk, gv, gt
 
 
@@ -374,11 +383,10 @@ def dense_transform_backward(grad_out: torch.Tensor, theta: torch.Tensor, kept: 
     gt = torch.empty_like(theta) if need_grad_theta else None
     with _on(dev):
         nbytes = _size(lib.pyg_dense_transform_backward_workspace, DTYPE[theta.dtype], N, Fi, Fo) if need_grad_theta else 0
-        if nbytes and (workspace is None or workspace.numel() < nbytes):
-            workspace = _workspace(nbytes, dev)
+        workspace = _room(workspace, nbytes, dev) if nbytes else None
         _check(lib.pyg_dense_transform_backward(_ptr(grad_out), DTYPE[theta.dtype], N, Fo, _ptr(theta), Fi,
                                                 _ptr(kept.codes) if kept else None, _ptr(kept.steps) if kept else None,
-                                                _ptr(gx), _ptr(gt), _ptr(workspace) if nbytes else None, nbytes,
+                                                _ptr(gx), _ptr(gt), _ptr(workspace), nbytes,
                                                 _stream(dev)), "pyg_dense_transform_backward")
     return gx, gt
 
@@ -505,10 +513,9 @@ def block_norm_backward(grad_r: torch.Tensor | None, grad_y: torch.Tensor | None
     grads = tuple(torch.empty_like(t) if t is not None and n else None for t, n in zip(tensors, need))
     with _on(h.device):
         nbytes = _bytes(lib.pyg_block_norm_backward_workspace, a)
-        if workspace is None or workspace.numel() < nbytes:
-            workspace = _workspace(nbytes, h.device)
+        workspace = _room(workspace, nbytes, h.device)
         _check(lib.pyg_block_norm_backward(ctypes.byref(a), _ptr(grad_r), _ptr(grad_y), *[_ptr(g) for g in grads],
-                                           _ptr(workspace), workspace.numel(), _stream(h.device)),
+                                           _ptr(workspace), nbytes, _stream(h.device)),
                "pyg_block_norm_backward")
     return grads
 

@@ -190,3 +190,30 @@ def test_calls_go_to_the_tensors_device(pyg, monkeypatch):
     assert len(seen) == 2 * 2 + (3 + 1 + 3) + 2 + 2 and all(seen)
     with pytest.raises(ValueError):
         pyg.DenseTransform.apply(gr, p["w_gate"])
+
+
+def test_workspaces_of_the_caller(pyg):
+    """Taken where they are large enough, in any type; refused where their bytes are not adjacent and
+    aligned; the same bits with what was in them before."""
+    p, gr, gy = params()
+    ptr = torch.tensor([0, 1], device="cuda")
+    q = torch.randn(1, 4, 16, device="cuda")
+    k, v = torch.randn(2, 3000, 4, 16, device="cuda")
+    k_ptr, table, lut = torch.tensor([0, 3000], device="cuda"), torch.randn(8, 4, device="cuda"), pyg.relative_buckets(8, 16)
+    x, w, go = torch.randn(300, 64, device="cuda"), torch.randn(64, 32, device="cuda"), torch.randn(300, 32, device="cuda")
+    one, kept = torch.ones(64, device="cuda"), pyg.activation_checkpoint(x)
+    stat = torch.empty(1, 4, 2, device="cuda")
+    out = pyg.global_attention(q, k, v, ptr, k_ptr, table, lut, stat=stat)
+    calls = (lambda ws: (pyg.global_attention(q, k, v, ptr, k_ptr, table, lut, workspace=ws),),
+             lambda ws: pyg.global_attention_backward(out, q, k, v, out, stat, ptr, k_ptr, table, lut, workspace=ws),
+             lambda ws: pyg.dense_transform_backward(go, w, kept, workspace=ws),
+             lambda ws: pyg.block_norm_backward(x, x, x, weight=one, bias=one, workspace=ws))
+    for call in calls:
+        want = call(None)
+        for fill in (0.0, float("nan")):
+            got = call(torch.full((1 << 22,), fill, device="cuda"))
+            assert all(a is b if a is None else torch.equal(a, b) for a, b in zip(want, got))
+        wide = torch.zeros(1 << 24, dtype=torch.uint8, device="cuda")
+        for bad in (wide[:1].expand(1 << 24), wide[::2], wide[4:], wide.cpu()):
+            with pytest.raises(ValueError):
+                call(bad)
