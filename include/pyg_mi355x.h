@@ -727,7 +727,8 @@ int pyg_dense_transform(const void *x, int x_dtype, int64_t N, int64_t Fi, const
  *   *_row, *_head  strides of a row and of a head in elements; features are adjacent.
  *   scale   factor c > 0 of the products.
  *   causal  non-zero: key j is seen by query i only where j <= i + nk - nq (positions in
- *           the graph; nk - nq aligns the last query with the last key).
+ *           the graph; nk - nq aligns the last query with the last key). Results and gradients of rows that
+ *           see only finite values are those, whatever (NaN, infinities) later rows hold.
  *   table   [buckets, H] in dtype, or NULL (no bias): T[b, h];
  *   bucket  int32 [2*reach+1]: the bucket of offset o - reach at place o (offsets
  *           beyond the reach take its ends' buckets). Entries outside [0, buckets) are

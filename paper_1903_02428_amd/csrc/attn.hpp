@@ -66,6 +66,15 @@ __device__ __forceinline__ bool flat(int first, int last, int reach, bool causal
     return last <= -reach || (first >= reach && !causal);
 }
 
+// The bias over c of offset d (key minus query) for head h, from memory, as stage_bias() makes it.
+template <typename T>
+__device__ __forceinline__ float bias_of(const Args &a, int h, int64_t d) {
+    if (!a.table) return 0.f;
+    int b = a.lut[d < -a.reach ? 0 : d > a.reach ? 2 * a.reach : static_cast<int>(d) + a.reach];
+    b = b < 0 ? 0 : b >= a.buckets ? a.buckets - 1 : b;
+    const float raw = to_f32(static_cast<const T *>(a.table)[(int64_t)b * a.H + h]);
+    return fabsf(raw) <= -kLowest ? fminf(fmaxf(raw * a.inv_scale, kLowest), -kLowest) : raw * a.inv_scale;
+}
 // The other half's value of the same column (lanes l and l ^ 32).
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
@@ -152,6 +161,105 @@ __device__ __forceinline__ void store_rows(T *out, int64_t row, bool there, int 
                 for (int i = 0; i < 4; ++i)
                     if (d + i < D) o[d + i] = T(v[i]);
             }
+        }
+}
+
+// ---- Causal calls whose later keys (or, for the keys' gradients, earlier queries) are not finite. Their weights are 0,
+// but 0 times them is NaN in the matrix cores, for every row of the tile that crosses the diagonal. The tile loops
+// let that happen: a wavefront that ends with results that are not finite looks whether they ought to be, and makes those
+// anew, value by value, that see nothing but finite ones. (Looking through the tiles in the loops made the
+// forward 4 to 14 % slower, without any such value; this takes nothing.)
+
+// The kernel's first argument from memory: what is read through it is not kept in scalar registers through the loops.
+template <typename A = Args>
+__device__ __forceinline__ const A &args_again() {
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *reinterpret_cast<const A *>((const void *)(p));
+}
+
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= -kLowest; }
+// Whether a word of two bf16 values or one fp32 value holds one that is not finite.
+template <typename T>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+    return (w & 0x7F800000u) == 0x7F800000u || (sizeof(T) == 2 && (w & 0x7F80u) == 0x7F80u);
+}
+template <typename T>
+__device__ __forceinline__ bool row_finite(const T *__restrict__ row, int D) {
+    bool fine = true;
+#pragma unroll 2
+    for (int d = 0; d < D; d += Elem<T>::E) {
+        const uint4 p = load_piece<T>(row, d, D, true);
+        fine = fine && !(not_finite<T>(p.x) || not_finite<T>(p.y) || not_finite<T>(p.z) || not_finite<T>(p.w));
+    }
+    return fine;
+}
+
+// Whether any of the results of a lane's column is not finite.
+template <int N>
+__device__ __forceinline__ bool column_odd(const f32x16 (&acc)[N]) {
+    float t = 0.f;  // 0 times each
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) t = fmaf(acc[i][r], 0.f, t);
+    t += other_half(t);
+    return t != t;
+}
+
+// Of the lanes with `flag`, those for which no row of first .. last that they see (seen(row)) fails fine(row), a lane a row.
+template <typename FINE, typename SEEN>
+__device__ __forceinline__ bool sees_only_fine(bool flag, int64_t first, int64_t last, int lane, FINE fine, SEEN seen) {
+#pragma unroll 1
+    for (int64_t j = first; j < last && __any(flag); j += kWave) {
+        uint64_t odd = __ballot(j + lane < last && !fine(j + lane));
+        for (; odd && __any(flag); odd &= odd - 1) flag = flag && !seen(j + __ffsll(static_cast<unsigned long long>(odd)) - 1);
+    }
+    return flag;
+}
+
+template <typename T>
+__device__ __forceinline__ float row_dot(const T *__restrict__ x, const T *__restrict__ y, int D) {
+    float t = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < D; d += Elem<T>::E) {
+        Piece<T> p, q;
+        p.u = load_piece<T>(x, d, D, true), q.u = load_piece<T>(y, d, D, true);
+#pragma unroll
+        for (int e = 0; e < Elem<T>::E; ++e) t = fmaf(to_f32(p.v[e]), to_f32(q.v[e]), t);
+    }
+    return t;
+}
+
+// Features d .. d + 3 of a row, zeros past D.
+template <typename T>
+__device__ __forceinline__ void load_four(const T *__restrict__ row, int d, int D, float (&v)[4]) {
+    typedef T four __attribute__((ext_vector_type(4)));
+    typedef four __attribute__((aligned(2))) any;
+    if (d + 4 <= D) {
+        const four x = *reinterpret_cast<const any *>(row + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = to_f32(x[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = d + i < D ? to_f32(row[d + i]) : 0.f;
+}
+
+// o += w row, a lane's features: 32 t + 8 (r / 4) + 4 h + r % 4 in o[t][r]. Nothing where w is 0, whatever the row holds.
+template <typename T, int DP>
+__device__ __forceinline__ void add_row(f32x16 (&o)[DP / 32], const T *__restrict__ row, float w, int D, int lane) {
+    w = to_f32(T(w));  // as the matrix cores take it
+    const int first = opaque(4 * (lane >> 5));
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int d = first + 32 * t + 8 * q;
+            float v[4];
+            load_four(row, d, D, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[t][4 * q + i] = w != 0.f ? fmaf(w, v[i], o[t][4 * q + i]) : o[t][4 * q + i];
         }
 }
 

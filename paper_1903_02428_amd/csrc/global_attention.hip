@@ -10,6 +10,41 @@ namespace {
 template <typename T, int DP, int WAVES>
 constexpr int kForwardWaves = DP <= 64 ? 2 : sizeof(T) == 2 ? 2 : 1;
 
+// Of a wavefront's rows, already stored, those that are not finite (flag) though they see nothing but finite values (see
+// attn.hpp). Everything but their maxima and sums is found out again: the tile loop keeps nothing for this.
+template <typename T, int DP, int WAVES>
+__device__ __forceinline__ void repair(int64_t nslots, float top, float mul, bool flag) {
+    const Args &a = args_again();
+    const int lane = opaque(threadIdx.x & 63), wave = to_scalar(threadIdx.x >> 6);
+    const uint32_t id = opaque(blockIdx.x);
+    const int hk = to_scalar(id % a.Hkv), head = to_scalar(hk * a.G + id / a.Hkv % a.G);
+    const Place pq = place_of(a.q_ptr, a.B, a.Nq, nslots - 1 - to_scalar(id / a.H), 32 * WAVES, 1, lane);
+    const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)), k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
+    const int64_t nk = k_last > k_first ? k_last - k_first : 0, i = (pq.tile * WAVES + wave) * 32 + (lane & 31);
+    const bool there = pq.first + i < pq.last;
+    const int64_t row = there ? pq.first + i : pq.first, shift = i + nk - (pq.last - pq.first);  // key j is at offset j - shift
+    const T *k = static_cast<const T *>(a.k) + hk * a.k_head + k_first * a.k_row;
+    const T *v = static_cast<const T *>(a.v) + hk * a.v_head + k_first * a.v_row;
+    const T *q = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
+    flag = sees_only_fine(flag && there, 0, nk, lane, [&](int64_t j) {
+        return row_finite(k + j * a.k_row, a.D) && row_finite(v + j * a.v_row, a.D);
+    }, [&](int64_t j) { return j <= shift; });
+    if (!__any(flag)) return;
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) o[t] = f32x16(0.f);
+#pragma unroll 1
+    for (int64_t j = 0; j < nk; ++j) {
+        const bool seen = flag && j <= shift;
+        if (!__any(seen)) continue;
+        const float s = row_dot(q, k + j * a.k_row, a.D) + bias_of<T>(a, head, j - shift);
+        add_row<T, DP>(o, v + j * a.v_row, seen ? __builtin_amdgcn_exp2f(a.c2 * (s - top)) : 0.f, a.D, lane);
+    }
+    store_rows<T, DP>(static_cast<T *>(a.out), row, flag, a.H, head, a.D, a.vec_o, o, mul, lane);
+    if constexpr (sizeof(T) == 2)
+        if (a.rest) store_rows<T, DP, true>(static_cast<T *>(a.rest), row, flag, a.H, head, a.D, a.vec_o, o, mul, lane);
+}
+
 // A workgroup owns 32 * WAVES queries of one graph and head and walks over the
 // graph's keys in tiles of BK, staged in LDS for its wavefronts; a wavefront
 // keeps 32 queries. S^T = K Q^T puts a query in a lane's column, so the running
@@ -165,6 +200,8 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         if (a.rest) store_rows<T, DP, true>(static_cast<T *>(a.rest), row, there, a.H, head, a.D, a.vec_o, acc, mul, lane);
     if (a.stat && there && h == 0)
         *reinterpret_cast<float2 *>(a.stat + (row * a.H + head) * 2) = make_float2(top, top == kNegInf ? 0.f : __log2f(sum));
+    const bool odd = column_odd(acc);
+    if (a.causal && __any(odd)) repair<T, DP, WAVES>(nslots, top, mul, odd);
 }
 
 template <typename T, int DP, int WAVES, int BK>

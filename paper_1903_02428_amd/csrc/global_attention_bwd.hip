@@ -13,6 +13,10 @@ namespace pyg {
 namespace attn {
 namespace {
 
+// Keys or queries a tile of four wavefronts.
+template <typename T, int DP>
+constexpr int kTileOfFour = DP * sizeof(T) <= 128 ? 64 : 32;
+
 // A row's statistics in units of s: p = exp2(c2 (s + start)), start = -(top + log2 sum / c2), -infinity for a row that
 // sees no key. bf16 tiles' accumulators begin with it, as dP's do with -delta; in fp32 that would round every
 // partial sum at start's magnitude (a table's gradient 1.3e-6 off instead of 4e-7), so it is added after the
@@ -25,6 +29,13 @@ struct RowStat {
 __device__ __forceinline__ RowStat row_stat(float2 s, float c2) {
     const float rest = -s.y / c2;
     return {s.x, s.x == kNegInf ? kNegInf : rest - s.x, rest};
+}
+
+// Statistics that are not finite (the row sees something that is not): its weights become infinite where it sees
+// something and stay 0 where it sees nothing, which NaN would not leave alone.
+constexpr float kHuge = -kLowest;
+__device__ __forceinline__ RowStat settled(const RowStat &s) {
+    return finite(s.start) || s.top == kNegInf ? s : RowStat{0.f, kHuge, kHuge};
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -46,7 +57,7 @@ __device__ __forceinline__ void lanes_meet() {
 // each, so that no two lanes add to one place: LDS float atomics, a lane at a time, made the
 // tiles near the diagonal a fifth of the kernel (three graphs, 9,001 nodes, 16 heads of 64).
 constexpr int kSkewRow = 40, kSkew = 32 * kSkewRow;  // 40: the two halves' rows are 32 banks apart
-__device__ __forceinline__ void add_diagonals(const f32x16 &ds, float *own, float *skew, int d0, int reach, int lane) {
+__device__ __forceinline__ void add_diagonals(const f32x16 &ds, float *own, float *skew, int d0, int reach, bool causal, int lane) {
     lane = opaque(lane);
     const int m = lane & 31, h = lane >> 5;
     lanes_meet();  // the last tile's reads
@@ -62,7 +73,8 @@ __device__ __forceinline__ void add_diagonals(const f32x16 &ds, float *own, floa
         t += static_cast<unsigned>(c) < 32u ? v : 0.f;
     }
     const int at = d0 + o;
-    const bool mine = lane < 63, low = mine && at < -reach, high = mine && at > reach;
+    const bool mine = lane < 63 && !(causal && at > 0);  // later keys: nothing, whatever their dP
+    const bool low = mine && at < -reach, high = mine && at > reach;
     if (mine && !low && !high) own[at + reach] += t;
     lanes_meet();  // the ends' sums, of whichever lane
     // the ends stand for all offsets beyond them
@@ -76,6 +88,61 @@ constexpr int kGradWaves = DP <= 64 || sizeof(T) == 2 ? 2 : 1;
 // The owned rows of V in LDS instead of registers: bf16 heads of 128 would need more than the 256 of two wavefronts a SIMD.
 template <typename T, int DP>
 constexpr bool kValuesInLds = DP == 128 && sizeof(T) == 2;
+
+// A row's statistics, and delta where its kernel has not stored it: g (out + rest).
+template <typename T>
+__device__ __forceinline__ RowStat stat_of(const Args &a, int64_t row, int head) {
+    return row_stat(*reinterpret_cast<const float2 *>(a.stat + (row * a.H + head) * 2), a.c2);
+}
+template <typename T>
+__device__ __forceinline__ float delta_of(const BackwardArgs &b, int64_t row, int head) {
+    const int64_t at = (row * b.f.H + head) * b.f.D;
+    const T *g = static_cast<const T *>(b.grad_out) + at, *o = static_cast<const T *>(b.f.out) + at;
+    const float d = row_dot(g, o, b.f.D);
+    return b.f.rest ? d + row_dot(g, static_cast<const T *>(b.f.rest) + at, b.f.D) : d;
+}
+
+// Of a wavefront's dQ, already stored, the rows that are not finite (flag) though they see nothing but finite values
+// (attn.hpp).
+template <typename T, int DP, int WAVES>
+__device__ __forceinline__ void repair_q(int64_t nslots, int splits, float *dq_part, bool flag) {
+    constexpr int BK = WAVES == 1 ? 32 : kTileOfFour<T, DP>;
+    const BackwardArgs &b = args_again<BackwardArgs>();
+    const Args &a = b.f;
+    const int lane = opaque(threadIdx.x & 63), wave = to_scalar(threadIdx.x >> 6);
+    const uint32_t id = opaque(blockIdx.x);
+    const int hk = to_scalar(id % a.Hkv), head = to_scalar(hk * a.G + id / a.Hkv % a.G), sp = to_scalar(id / a.H % splits);
+    const Place pq = place_of(a.q_ptr, a.B, a.Nq, nslots - 1 - to_scalar(id / a.H / splits), 32 * WAVES, 1, lane);
+    const int64_t k_first = uniform64(ptr_at(a.k_ptr, pq.graph, a.Nk)), k_last = uniform64(ptr_at(a.k_ptr, pq.graph + 1, a.Nk));
+    const int64_t nk = k_last > k_first ? k_last - k_first : 0, i = (pq.tile * WAVES + wave) * 32 + (lane & 31);
+    const bool there = pq.first + i < pq.last;
+    const int64_t row = there ? pq.first + i : pq.first, shift = i + nk - (pq.last - pq.first);
+    const T *k = static_cast<const T *>(a.k) + hk * a.k_head + k_first * a.k_row;
+    const T *v = static_cast<const T *>(a.v) + hk * a.v_head + k_first * a.v_row;
+    const T *q = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head;
+    const T *g = static_cast<const T *>(b.grad_out) + (row * a.H + head) * a.D;
+    const RowStat st = stat_of<T>(a, row, head);
+    const float delta = delta_of<T>(b, row, head);
+    flag = flag && there && row_finite(q, a.D) && row_finite(g, a.D);
+    flag = sees_only_fine(flag, 0, nk, lane, [&](int64_t j) {
+        return row_finite(k + j * a.k_row, a.D) && row_finite(v + j * a.v_row, a.D);
+    }, [&](int64_t j) { return j <= shift; });
+    if (!__any(flag)) return;
+    const int64_t share = splits > 1 ? ((nk + BK - 1) / BK + splits - 1) / splits * BK : nk;  // the workgroup's keys
+    const int64_t last = (sp + 1) * share < nk ? (sp + 1) * share : nk;
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) o[t] = f32x16(0.f);
+#pragma unroll 1
+    for (int64_t j = sp * share; j < last; ++j) {
+        const bool seen = flag && j <= shift && st.top != kNegInf;
+        if (!__any(seen)) continue;
+        const float s = row_dot(q, k + j * a.k_row, a.D) + bias_of<T>(a, head, j - shift), dp = row_dot(g, v + j * a.v_row, a.D);
+        add_row<T, DP>(o, k + j * a.k_row, seen ? __builtin_amdgcn_exp2f(a.c2 * ((s - st.top) + st.rest)) * (dp - delta) : 0.f, a.D, lane);
+    }
+    if (splits > 1) store_rows<float, DP>(dq_part, row, flag, a.H, head, a.D, a.D % 4 == 0, o, a.scale, lane);
+    else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, flag, a.H, head, a.D, a.vec_o, o, a.scale, lane);
+}
 
 // A workgroup owns 32 * WAVES queries, as in the forward.
 template <typename T, int DP, int WAVES, int BK>
@@ -167,10 +234,12 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         raw = *reinterpret_cast<const float2 *>(a.stat + (row * a.H + head) * 2);
         if (h == 0 && sp == 0) delta[row * a.H + head] = dl;
     }
-    const RowStat st = row_stat(raw, a.c2);
+    RowStat st = row_stat(raw, a.c2);
+    if (!finite(dl)) st.start = dl, dl = 0.f;  // an infinite P leaves dS as little finite, where anything is seen
+    st = settled(st);
     constexpr bool kDeltaFirst = DP < 128 && !kStartLate<T>;  // dP starts from it, but where registers are short
     const f32x16 no_delta(-dl);
-    const float late = kStartLate<T> && !wild ? a.c2 * st.start : 0.f;
+    const float late = kStartLate<T> && !wild ? fminf(a.c2 * st.start, kHuge) : 0.f;
 
     registers_loaded();
     f32x16 acc[DP / 32];
@@ -214,6 +283,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
                     for (int r = 0; r < 16; ++r) s[n][r] = st.top == kNegInf ? kNegInf : (s[n][r] - st.top) + st.rest;
                 }
                 mask_tile<true>(s[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)  // whatever dP is where nothing is seen
+                    dp[n][r] = s[n][r] == kNegInf ? (kDeltaFirst ? 0.f : dl) : dp[n][r];
             }
         }
 #pragma unroll
@@ -232,7 +304,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
                 (d0 > 0 ? above : below) += t;
             } else {
 #pragma unroll
-                for (int n = 0; n < NK; ++n) add_diagonals(s[n], own, skew, d0 + 32 * n, a.reach, lane);
+                for (int n = 0; n < NK; ++n) add_diagonals(s[n], own, skew, d0 + 32 * n, a.reach, a.causal, lane);
             }
         }
 #pragma unroll
@@ -270,6 +342,8 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     if (b.grad_q) {
         if (splits > 1) store_rows<float, DP>(dq_part, row, there, a.H, head, a.D, a.D % 4 == 0, acc, a.scale, lane);
         else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
+        const bool odd = column_odd(acc);
+        if (a.causal && __any(odd)) repair_q<T, DP, WAVES>(nslots, splits, dq_part, odd);
     }
     if (mine) {
         below = wave_sum(below), above = wave_sum(above);
@@ -285,6 +359,66 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
             }
             mine[i] = t;
         }
+    }
+}
+
+// The same of dK and dV: keys whose gradients are not finite (flag) though every query that sees them, over the heads that
+// the workgroup has, is finite with its gradient and its statistics.
+template <typename T, int DP, int WAVES>
+__device__ __forceinline__ void repair_kv(const float *__restrict__ delta, int splits, float *__restrict__ part, bool flag) {
+    const BackwardArgs &b = args_again<BackwardArgs>();
+    const Args &a = b.f;
+    const int lane = opaque(threadIdx.x & 63), wave = to_scalar(threadIdx.x >> 6);
+    const uint32_t id = opaque(blockIdx.x);
+    const int hk = to_scalar(id % a.Hkv), heads = a.G / splits, first = hk * a.G + to_scalar(id / a.Hkv % splits) * heads;
+    const Place pk = place_of(a.k_ptr, a.B, a.Nk, to_scalar(id / a.Hkv / splits), 32 * WAVES, 1, lane);
+    const int64_t q_first = uniform64(ptr_at(a.q_ptr, pk.graph, a.Nq)), q_last = uniform64(ptr_at(a.q_ptr, pk.graph + 1, a.Nq));
+    const int64_t nq = q_last > q_first ? q_last - q_first : 0, j = (pk.tile * WAVES + wave) * 32 + (lane & 31);
+    const bool there = pk.first + j < pk.last;
+    const int64_t row = there ? pk.first + j : pk.first, shift = j - (pk.last - pk.first - nq);  // query i is at offset shift - i
+    const T *k = static_cast<const T *>(a.k) + row * a.k_row + hk * a.k_head;
+    const T *v = static_cast<const T *>(a.v) + row * a.v_row + hk * a.v_head;
+    const auto q_of = [&](int64_t i, int head) { return static_cast<const T *>(a.q) + (q_first + i) * a.q_row + head * a.q_head; };
+    const auto g_of = [&](int64_t i, int head) { return static_cast<const T *>(b.grad_out) + ((q_first + i) * a.H + head) * a.D; };
+    flag = flag && there && row_finite(k, a.D) && row_finite(v, a.D);
+#pragma unroll 1
+    for (int head = first; head < first + heads && __any(flag); ++head)
+        flag = sees_only_fine(flag, 0, nq, lane, [&](int64_t i) {
+            const RowStat st = stat_of<T>(a, q_first + i, head);
+            return row_finite(q_of(i, head), a.D) && row_finite(g_of(i, head), a.D) &&
+                   (st.top == kNegInf || finite(st.start)) && finite(delta[(q_first + i) * a.H + head]);
+        }, [&](int64_t i) { return i >= shift; });
+    if (!__any(flag)) return;
+    const auto walk = [&](auto visit) {
+#pragma unroll 1
+        for (int head = first; head < first + heads; ++head)
+#pragma unroll 1
+            for (int64_t i = 0; i < nq; ++i) {
+                const RowStat st = stat_of<T>(a, q_first + i, head);
+                const bool seen = flag && i >= shift && st.top != kNegInf;
+                if (__any(seen)) {
+                    const float s = row_dot(q_of(i, head), k, a.D) + bias_of<T>(a, head, shift - i);
+                    visit(i, head, seen ? __builtin_amdgcn_exp2f(a.c2 * ((s - st.top) + st.rest)) : 0.f);
+                }
+            }
+    };
+    // dV, then dK
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        f32x16 o[DP / 32];
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) o[t] = f32x16(0.f);
+        walk([&](int64_t i, int head, float p) {
+            const T *row = g_of(i, head);
+            if (which) {
+                p = p != 0.f ? p * (row_dot(row, v, a.D) - delta[(q_first + i) * a.H + head]) : 0.f;
+                row = q_of(i, head);
+            }
+            add_row<T, DP>(o, row, p, a.D, lane);
+        });
+        const float mul = which ? a.scale : 1.f;
+        if (splits > 1) store_rows<float, DP>(which ? part : part + a.Nk * a.Hkv * a.D, row, flag, a.Hkv, hk, a.D, a.D % 4 == 0, o, mul, lane);
+        else store_rows<T, DP>(static_cast<T *>(which ? b.grad_k : b.grad_v), row, flag, a.Hkv, hk, a.D, a.vec_o, o, mul, lane);
     }
 }
 
@@ -371,9 +505,9 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             sg.load(gb, i0, nq - i0, lds + (2 * half + 1) * kTile);
         };
         auto put = [&](int64_t i0, int half) {
-            const RowStat t = row_stat(make_float2(i0 + query < nq ? next.x : kNegInf, next.y), a.c2);
+            const RowStat t = settled(row_stat(make_float2(i0 + query < nq ? next.x : kNegInf, next.y), a.c2));
             float *s = stats + half * 4 * BQ + query;
-            s[0] = t.start, s[BQ] = -next_delta, s[2 * BQ] = t.top, s[3 * BQ] = t.rest;  // the same from several threads
+            s[0] = t.start, s[BQ] = i0 + query < nq ? -next_delta : 0.f, s[2 * BQ] = t.top, s[3 * BQ] = t.rest;  // the same from several threads
         };
         // one form for all tiles, its accumulators being most of the registers: inner tiles jump over what they do not need
         auto step = [&](const char *qt, const char *gt, const float *stat, int64_t i0) {
@@ -424,6 +558,11 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
                         }
                     }
                     mask_tile<false>(s[n], keys, left - 32 * n, a.causal, d0 - 32 * n, lane);
+                    if constexpr (!kStartLate<T>) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)  // whatever dP is where nothing is seen
+                            dp[n][r] = s[n][r] == kNegInf ? 0.f : dp[n][r];
+                    }
                 }
             }
 #pragma unroll
@@ -435,6 +574,12 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
                     s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, e, constant));
                     dp[n][r] = s[n][r] * (kStartLate<T> ? dp[n][r] + at[BQ] : dp[n][r]);  // dS
                 }
+            if (kStartLate<T> && !inner && a.causal) {  // the same, with its late delta
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dp[n][r] = s[n][r] == 0.f ? 0.f : dp[n][r];
+            }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -465,6 +610,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
         }
     }
+    const bool odd = column_odd(dk) || column_odd(dv);
     if (splits > 1) {
         store_rows<float, DP>(dk_part, row, there, a.Hkv, hk, a.D, a.D % 4 == 0, dk, a.scale, lane);
         store_rows<float, DP>(dv_part, row, there, a.Hkv, hk, a.D, a.D % 4 == 0, dv, 1.f, lane);
@@ -472,6 +618,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
         store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
         store_rows<T, DP>(static_cast<T *>(b.grad_v), row, there, a.Hkv, hk, a.D, a.vec_o, dv, 1.f, lane);
     }
+    if (a.causal && __any(odd)) repair_kv<T, DP, WAVES>(delta, splits, dk_part, odd);
 }
 
 // dK and dV from the shares of the head groups [splits][2][Nk, Hkv, D], in order.
@@ -600,7 +747,7 @@ int launch_kv(const BackwardArgs &b, const Plan &p, const Buffers &w, hipStream_
 template <typename T, int DP>
 int launch(const BackwardArgs &b, void *ws, hipStream_t s) {
     const Args &a = b.f;
-    constexpr int BK = DP * sizeof(T) <= 128 ? 64 : 32;  // keys or queries a tile of four wavefronts
+    constexpr int BK = kTileOfFour<T, DP>;
     const Wanted want{b.grad_q != nullptr, b.grad_k != nullptr, b.grad_table != nullptr};
     const Plan p = plan_of(a, want);
     if (p.q_slots * a.H * p.q_splits * (p.lone_q ? 64 : 256) > kMost || p.kv_slots * a.Hkv * p.kv_splits * (p.lone_kv ? 64 : 256) > kMost)

@@ -145,6 +145,54 @@ __device__ __forceinline__ void put(const Args &a, int64_t at, float v) {
         if (a.rest) static_cast<T *>(a.rest)[at] = T(v - to_f32(r));
 }
 
+// Of a wavefront's results, before they are divided by the sums, the rows that are not finite (flag) though they see
+// nothing but finite values among the workgroup's keys (attn.hpp).
+template <typename T, int DP>
+__device__ __forceinline__ void repair(int64_t nslots, int splits, float top, bool flag, f32x4 (&acc)[DP / 16]) {
+    using F = Few<T, DP>;
+    const Args &a = args_again();
+    const int lane = opaque(threadIdx.x & 63), wave = to_scalar(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+    const uint32_t id = opaque(blockIdx.x);
+    const int hk = to_scalar(id % a.Hkv), sp = to_scalar(id / a.Hkv % splits);
+    const Place p = place_of(a.q_ptr, a.B, a.Nq, to_scalar(id / a.Hkv / splits), 16, a.G, lane);
+    const int64_t k_first = uniform64(ptr_at(a.k_ptr, p.graph, a.Nk)), k_last = uniform64(ptr_at(a.k_ptr, p.graph + 1, a.Nk));
+    const int64_t nk = k_last > k_first ? k_last - k_first : 0, nq = p.last - p.first, rr = p.tile * 16 + m;
+    const bool there = rr < nq * a.G;
+    const int64_t i = there ? rr / a.G : 0, shift = i + nk - nq;
+    const int head = hk * a.G + static_cast<int>(rr % a.G);
+    const T *k = static_cast<const T *>(a.k) + k_first * a.k_row + hk * a.k_head;
+    const T *v = static_cast<const T *>(a.v) + k_first * a.v_row + hk * a.v_head;
+    const T *q = static_cast<const T *>(a.q) + (p.first + i) * a.q_row + head * a.q_head;
+    const int64_t len = (nk + splits - 1) / splits, begin = len * sp, end = begin + len < nk ? begin + len : nk;
+    flag = sees_only_fine(flag && there, begin, end, lane, [&](int64_t j) {
+        return row_finite(k + j * a.k_row, a.D) && row_finite(v + j * a.v_row, a.D);
+    }, [&](int64_t j) { return j <= shift; });
+    if (!__any(flag)) return;
+    f32x4 o[F::W];
+#pragma unroll
+    for (int t = 0; t < F::W; ++t) o[t] = f32x4(0.f);
+#pragma unroll 1
+    for (int64_t j = begin + wave * F::KEYS; j < end; j += (j - begin + 1) % F::KEYS ? 1 : (kFewWaves - 1) * F::KEYS + 1) {  // the wavefront's own
+        const bool seen = flag && j <= shift;
+        if (!__any(seen)) continue;
+        const float s = row_dot(q, k + j * a.k_row, a.D) + bias_of<T>(a, head, j - shift);
+        const float w = to_f32(T(seen ? __builtin_amdgcn_exp2f(a.c2 * (s - top)) : 0.f));  // as the matrix cores take it
+        const int first = opaque(4 * g * F::W);
+#pragma unroll
+        for (int t = 0; t < F::W; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = first + r * F::W + t;
+                const float x = to_f32(v[j * a.v_row + (d < a.D ? d : 0)]);  // past D: not kept
+                o[t][r] = w != 0.f ? fmaf(w, x, o[t][r]) : o[t][r];
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < F::W; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[t][r] = flag ? o[t][r] : acc[t][r];
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t nslots, int splits, float *__restrict__ part) {
     using F = Few<T, DP>;
@@ -184,16 +232,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
     const int64_t len = (nk + splits - 1) / splits, begin = len * sp;
     const int64_t end = begin + len < nk ? begin + len : nk;
     const int64_t shift = rr / a.G + nk - nq;  // offset of key j and the lane's query: j - shift
-    const T *table = static_cast<const T *>(a.table);
-    auto bias_at = [&](int64_t d) {
-        const int o = d < -a.reach ? 0 : d > a.reach ? 2 * a.reach : static_cast<int>(d) + a.reach;
-        int b = a.lut[o];
-        b = b < 0 ? 0 : b >= a.buckets ? a.buckets - 1 : b;
-        const float raw = to_f32(table[(int64_t)b * a.H + head]);
-        return fabsf(raw) <= -kLowest ? fminf(fmaxf(raw * a.inv_scale, kLowest), -kLowest) : raw * a.inv_scale;
-    };
-    const bool biased = table && there;
-    const float far = biased ? bias_at(-a.reach) : 0.f;
+    const bool biased = a.table && there;
+    const float far = biased ? bias_of<T>(a, head, -a.reach) : 0.f;
 
     f32x4 acc[W];
 #pragma unroll
@@ -212,7 +252,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
         for (int u = 0; u < F::SUB; ++u) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                s[u][r] = !biased ? 0.f : is_far ? far : bias_at(j + 16 * u + 4 * g + r - shift);
+                s[u][r] = !biased ? 0.f : is_far ? far : bias_of<T>(a, head, j + 16 * u + 4 * g + r - shift);
 #pragma unroll
             for (int i = 0; i < F::STEPS; ++i) {
                 Piece<T> x, y;
@@ -273,6 +313,16 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
                     acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(cur.v[r][i]), s[0][r], acc[i], 0, 0, 0);
         }
         cur = next;
+    }
+    if (a.causal) {
+        float odd = 0.f;  // 0 times each of the column's results
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) odd = fmaf(acc[i][r], 0.f, odd);
+        odd += __shfl_xor(odd, 16);
+        odd += __shfl_xor(odd, 32);
+        if (__any(odd != odd)) repair<T, DP>(nslots, splits, top, odd != odd, acc);
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);

@@ -205,3 +205,82 @@ def test_captured_with_a_workspace_that_others_write(pyg):  # noqa: F811
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip((*grads, out), want))
+
+
+HIDDEN = [  # queries, keys, heads, key heads, features: every form, causal
+    ([2, 5], [40, 300], 2, 1, 24),
+    ([1], [600], 2, 2, 32),
+    ([2, 3], [1100, 2050], 2, 1, 128),
+    ([33, 20, 70], None, 2, 1, 16),
+    ([40, 90], [70, 60], 2, 2, 80),
+    ([300, 200], None, 2, 1, 64),
+    ([260], None, 2, 1, 128),
+    ([1100], [1150], 2, 1, 32),
+    ([1040], None, 2, 1, 128),
+    ([1100], None, 1, 1, 64),
+    ([30, 45], None, 2, 1, 7),
+    ([3], [70], 2, 2, 33),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("i", range(len(HIDDEN)))
+def test_what_a_row_does_not_see_may_be_anything(pyg, i, dtype):  # noqa: F811
+    """NaN and infinities in a key, value, query or gradient reach what sees them and nothing else: results in
+    which they have no part are those of clean inputs, the rows in which they have one are not finite."""
+    qn, kn, H, Hkv, D = HIDDEN[i]
+    same = kn is None
+    kn = qn if same else kn
+    reach = 6
+    q, k, v, grad, _, _ = inputs(400 + i, qn, kn, H, Hkv, D, DT[dtype], 0, 0, True, pyg)
+    lut = torch.arange(2 * reach + 1, dtype=torch.int32)  # a bucket for every offset, the later keys' unused
+    table = torch.randn(2 * reach + 1, H, generator=torch.Generator().manual_seed(i)).to(DT[dtype])
+    M = torch.zeros(sum(qn), sum(kn), dtype=torch.bool)  # whether query i sees key j
+    i0 = j0 = 0
+    for n, m in zip(qn, kn):
+        M[i0:i0 + n, j0:j0 + m] = torch.arange(m)[None] <= torch.arange(m - n, m)[:, None]
+        i0, j0 = i0 + n, j0 + m
+    ref = attention(q, k, v, qn, kn, table, lut, True, grad=grad)
+
+    def call(q, k, v, g):
+        got = run(pyg, q, k, v, g, table, lut, qn, kn, True, same=same)
+        assert (got["grad_table"][reach + 1:] == 0).all()  # offsets that no row sees
+        return {n: t.cpu() for n, t in got.items()}
+
+    def others(got, x, part, what):
+        close({x: got[x][~part]}, {x: tuple(t[~part] for t in ref[x])}, str(what))
+
+    def odd(t):
+        return not torch.isfinite(t).all(2).any()
+    clean = call(q, k, v, grad)
+    close(clean, ref, "clean")
+    for j in (kn[0] - 1, max(kn[0] - 3, 0), sum(kn) - 1 - kn[-1] // 2):
+        rows = M[:, j]
+        beside = M[rows].any(0)  # keys seen by a row that sees key j
+        for value in ("k", math.nan, math.inf, -math.inf):
+            bad_k, bad_v = k.clone(), v.clone()
+            if value == "k":
+                bad_k[j, :, 1] = math.nan
+            else:
+                bad_v[j, :, 1] = value
+            got = call(q, bad_k, bad_v, grad)
+            for x, part in (("out", rows), ("grad_q", rows), ("grad_k", beside), ("grad_v", beside & (value == "k"))):
+                others(got, x, part, (value, j))
+            assert odd(got["out"][rows]) and odd(got["grad_q"][rows]) and odd(got["grad_k"][beside])
+    for r in (min(2, qn[0] - 1), sum(qn) - 1 - qn[-1] // 2):
+        rows, keys = torch.arange(sum(qn)) == r, M[r]
+        for value in ("q", math.nan, math.inf):
+            bad_q, bad_g = q.clone(), grad.clone()
+            if value == "q":
+                bad_q[r, :, 1] = math.nan
+            else:
+                bad_g[r, :, 1] = value
+            got = call(bad_q, k, v, bad_g)
+            sees = rows & bool(keys.any())  # a row that sees nothing has zeros whatever it holds
+            for x, part in (("out", sees & (value == "q")), ("grad_q", sees), ("grad_k", keys), ("grad_v", keys)):
+                others(got, x, part, (value, r))
+            assert odd(got["grad_q"][sees]) and odd(got["grad_k"][keys]) and odd(got["grad_v"][keys])
+    # and all of it at once, which ends
+    nan = [torch.full_like(t, math.nan) for t in (q, k, v, grad)]
+    got = call(*nan)
+    assert odd(got["out"][M.any(1)]) and odd(got["grad_q"][M.any(1)]) and odd(got["grad_k"][M.any(0)]) and odd(got["grad_v"][M.any(0)])
