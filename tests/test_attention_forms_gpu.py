@@ -94,7 +94,7 @@ def test_no_leak_between_graphs_in_every_form(pyg, qn, kn, dtype):  # noqa: F811
 REST = [  # queries, keys, causal: every form of the forward and of dQ
     ([1, 2], [37, 300], False),
     ([1], [600], False),
-    ([1, 2], [1030, 1100], True),
+    ([3], [1030], True),
     ([33, 20, 60], [33, 20, 60], True),
     ([200, 129], [200, 129], False),
     ([1100], [40], False),
@@ -105,7 +105,7 @@ def flat(qn, kn, causal):
     """Inputs whose rows weigh all the keys they see alike (q is 0), with values far from 0 beside their spread, and
     the weights: P is 1 / n, its parts in bf16 exact, so that nothing but the result's own rounding is lost."""
     g = torch.Generator().manual_seed(17)
-    H, D = 2, 32
+    H, D = 2, 8
     q = torch.zeros(sum(qn), H, D).bfloat16()
     k, v = ((torch.randn(sum(kn), H, D, generator=g) * s + o).bfloat16() for s, o in ((1, 4), (0.25, 16)))
     grad = torch.randn(sum(qn), H, D, generator=g).bfloat16()
@@ -120,14 +120,14 @@ def flat(qn, kn, causal):
 
 @pytest.mark.parametrize("qn,kn,causal", REST)
 def test_rest_is_what_rounding_took(pyg, qn, kn, causal):  # noqa: F811
-    """out + rest is the result to 16 bits more than out: the mean of the values. It is off by
-    rest's own rounding, 2^-9 of at most 2^-9 of the result, by a sum of n terms and its division."""
+    """out + rest is the result to 8 bits more than out: the mean of the values. It is off by
+    rest's own rounding, half a step (2^-8) of at most half a step of the result, by a sum of n terms and its division."""
     q, k, v, _, P = flat(qn, kn, causal)
     rest = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
     out = pyg.global_attention(q.cuda(), k.cuda(), v.cuda(), ptr_of(qn), ptr_of(kn), causal=causal, rest=rest).cpu().double()
     rest = rest.cpu().double()
     want = torch.einsum("ij,jhd->ihd", P, v.double())
-    bound = ((max(kn) + 4) * U32 + 2.0 ** -18) * 1.01 * want.abs()  # the magnitudes' mean: values are positive
+    bound = ((max(kn) + 4) * U32 + 2.0 ** -16) * 1.01 * want.abs()  # the magnitudes' mean: values are positive
     assert (v > 0).all() and ((out + rest - want).abs() <= bound).all()
     for wrong in (0.0, -1.0):
         assert ((out + wrong * rest - want).abs() > bound).any()
@@ -140,7 +140,7 @@ def test_rest_reaches_the_gradients(pyg, qn, kn, causal):  # noqa: F811
     way round, grad_q lies outside them (and the table's gradient, where it is the sum of few rows and keys)."""
     q, k, v, grad, P = flat(qn, kn, causal)
     H, D = q.shape[1:]
-    c, n, half = D ** -0.5, max(kn), 2.0 ** -9
+    c, n, half = D ** -0.5, max(kn), torch.finfo(torch.bfloat16).eps / 2
     table, lut = torch.zeros(4, H).bfloat16(), pyg.relative_buckets(4, 8, True, "cpu")
     R = len(lut) // 2
     g, x, y = grad.double(), k.double(), v.double()
@@ -148,7 +148,7 @@ def test_rest_reaches_the_gradients(pyg, qn, kn, causal):  # noqa: F811
     dp = torch.einsum("ihd,jhd->hij", g, y)
     mag = torch.einsum("ihd,jhd->hij", g.abs(), y.abs())
     delta = (g * o).sum(2).T[:, :, None]
-    derr = (g.abs() * o.abs()).sum(2).T[:, :, None] * (2.0 ** -18 * 1.01 + (n + 4 + D + 2) * U32)
+    derr = (g.abs() * o.abs()).sum(2).T[:, :, None] * (2.0 ** -16 * 1.01 + (n + 4 + D + 2) * U32)
     ds = P * (dp - delta)
     dserr = P * ((n + 16) * U32 * (dp - delta).abs() + (D + 2) * U32 * mag + derr)
     dsr = dserr + half * (ds.abs() + dserr)
