@@ -758,7 +758,7 @@ int pyg_global_attention_workspace(const pyg_attention *a, size_t *bytes);
  *   q [Nq, H, D], k and v [Nk, Hkv, D] with the strides of *a; out [Nq, H, D] contiguous;
  *   stat  fp32 [Nq, H, 2] or NULL: what the backward needs of every row;
  *   rest  [Nq, H, D] or NULL, bf16 only: what rounding took from out (the backward's row sums are
- *         as exact with it as if out had 16 bits more).
+ *         as exact with it as if out had 8 bits more).
  * A row that sees no key (none in its graph, all masked, all entries -infinity)
  * gives zeros, and zero gradients. Scores, sums and statistics are fp32; bf16
  * weights p are rounded to bf16 for the second product. Deterministic.
@@ -774,7 +774,8 @@ int pyg_global_attention_backward_workspace(const pyg_attention *a, size_t *byte
 
 /* Gradients of the above from grad_out [Nq, H, D], the inputs, `out`, `stat` and `rest` (or
  * NULL) of the forward: grad_q [Nq, H, D], grad_k and grad_v [Nk, Hkv, D] (summed over the heads that
- * share a key head in fp32), grad_table [buckets, H] or NULL, all contiguous, in dtype. Those that
+ * share a key head in fp32), grad_table [buckets, H] or NULL, all contiguous, in dtype. bf16: the weights p and
+ * their gradients are rounded to bf16 for the products. Those that
  * a->skip names are neither made nor written (NULL may stand for them).
  * Rows of no graph get zeros. Deterministic. Errors: as above. */
 int pyg_global_attention_backward(const pyg_attention *a, const void *grad_out, const void *q, const void *k,

@@ -1,7 +1,8 @@
 // Activations in 8 bits: blocks of 32 features of a row share a step, a power
 // of two: the smallest that leaves the block's largest magnitude below 127.5
 // steps. A value is its nearest multiple of the step (ties to even), so the error
-// is at most half a step, 2^-7 of the largest magnitude of the block at most.
+// is at most half a step: 1 / 127.5 of the block's largest magnitude at most, or 2^-127
+// where the step is the smallest.
 // Everything is exact but that one rounding: x / step is a change of exponent,
 // and code * step has 7 significant bits, so it is a bf16 value too, which
 // lets the gradient's product take the codes to the matrix cores unrounded.

@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
                 sum += s[u][r];
             }
         if constexpr (F::kBf16) {
-            Piece<T> pp;
+            Piece<T> pp;  // P rounded to bf16, as in the tiled forward
             pp.u = make_uint4(pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]), pack_bf16(s[1][0], s[1][1]),
                               pack_bf16(s[1][2], s[1][3]));
 #pragma unroll

@@ -199,3 +199,11 @@ def test_parts_of_extreme_values(pyg):
     _, gt = pyg.dense_transform_backward(torch.cat([nan[:1], torch.ones(2, 1)]).cuda(), torch.ones(32, 1, device="cuda"),
                                          pyg.activation_checkpoint(x.cuda()))
     assert torch.isnan(gt).all()
+
+
+def test_largest_error_of_a_block(pyg):
+    """Half a step is up to 1 / 127.5 of a block's largest magnitude: 127.5 takes steps of 2, and 1 comes back as 0."""
+    x = torch.full((2, 32), 1.0)
+    x[0, 0], x[1, 0] = 127.5, 127.4375
+    got = pyg.checkpoint_restore(pyg.activation_checkpoint(x.cuda())).cpu()
+    assert (got[0, 1:] == 0).all() and got[0, 0] == 128 and torch.equal(got[1], torch.tensor([127.0] + [1.0] * 31))
