@@ -803,7 +803,7 @@ typedef struct {
 } pyg_block_norm_args;
 
 /* r and y [N, F] in dtype, each rounded once (y is taken of the unrounded r; r may be NULL
- * where y is made). codes and steps, or NULL: y as it was stored, in 8 bits (see
+ * where y is made). codes (16-byte aligned) and steps, or NULL: y as it was stored, in 8 bits (see
  * pyg_activation_checkpoint). Statistics are fp32, two-pass. Deterministic.
  * Errors: PYG_ERR_INVALID_ARG (bad dtype or norm, missing arrays, y without weight or
  * weight without y, codes without y, eps < 0, results that overlap the inputs or one another), PYG_ERR_UNSUPPORTED (F > 8192, N >= 2^31). */

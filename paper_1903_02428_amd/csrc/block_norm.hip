@@ -575,7 +575,7 @@ extern "C" int pyg_block_norm(const pyg_block_norm_args *c, void *r, void *y, in
     if ((codes == nullptr) != (steps == nullptr) || (!c->weight && (y || codes))) return PYG_ERR_INVALID_ARG;
     if (c->weight && !y && c->N > 0) return PYG_ERR_INVALID_ARG;
     if (c->N == 0) return PYG_OK;
-    if (!c->h || (!r && !y)) return PYG_ERR_INVALID_ARG;
+    if (!c->h || (!r && !y) || reinterpret_cast<uintptr_t>(codes) % 16) return PYG_ERR_INVALID_ARG;
     const int64_t all = c->N * c->F * (c->dtype == PYG_BF16 ? 2 : 4), blocks = c->N * ((c->F + 31) / 32);
     const Span results[] = {{r, all}, {y, all}, {codes, blocks * 32}, {steps, blocks}};
     if (!apart(results, inputs_of(c).s)) return PYG_ERR_INVALID_ARG;

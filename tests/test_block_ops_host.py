@@ -280,3 +280,9 @@ def test_dense_sizes_are_refused_before_anything_is_launched(lib):
         return lib.pyg_dense_transform_backward(A, 0, N, Fo, B_, Fi, C_, C_, gx, gt, D_, 1 << 62, None)
     assert rc(1, 1 << 23, 1 << 23, D_, A) == UNSUPPORTED and rc(1, 1 << 23, 1 << 23, None, A) == UNSUPPORTED
     assert rc((1 << 31) - 1, 1 << 23, 1, D_, None) == UNSUPPORTED
+
+
+def test_block_norm_codes_lie_on_16_bytes(lib):
+    """As the other calls that read and write them want it."""
+    a = norm()
+    assert lib.pyg_block_norm(ctypes.byref(a), at(1 << 30), at(2 << 30), at((3 << 30) + 8), at(4 << 30), None) == INVALID
