@@ -111,9 +111,10 @@ __device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int d0
 }
 
 // -infinity where there is no such key (rows from `keys` on) or it comes later
-// than the query (causal, offset > 0).
-template <bool KEYS_IN_ROWS>
-__device__ __forceinline__ void mask_tile(f32x16 &c, int keys, int queries, bool causal, int d0, int lane) {
+// than the query (causal, offset > 0); in the backward `none` for dP there, whatever it is.
+template <bool KEYS_IN_ROWS, bool BACKWARD = false>
+__device__ __forceinline__ void mask_tile(f32x16 &c, int keys, int queries, bool causal, int d0, int lane, f32x16 *dp = nullptr,
+                                          float none = 0.f) {
     if (keys >= 32 && queries >= 32 && (!causal || d0 + 31 <= 0)) return;
     lane = opaque(lane);
     const int m = lane & 31, h = lane >> 5;
@@ -121,7 +122,10 @@ __device__ __forceinline__ void mask_tile(f32x16 &c, int keys, int queries, bool
     for (int r = 0; r < 16; ++r) {
         const int row = 8 * (r >> 2) + 4 * h + (r & 3);
         const int key = KEYS_IN_ROWS ? row : m, query = KEYS_IN_ROWS ? m : row;
-        if (key >= keys || query >= queries || (causal && d0 + key - query > 0)) c[r] = kNegInf;
+        if (key >= keys || query >= queries || (causal && d0 + key - query > 0)) {
+            c[r] = kNegInf;
+            if constexpr (BACKWARD) (*dp)[r] = none;
+        }
     }
 }
 

@@ -285,10 +285,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[n][r] = st.top == kNegInf ? kNegInf : (s[n][r] - st.top) + st.rest;
                 }
-                mask_tile<true>(s[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)  // whatever dP is where nothing is seen
-                    dp[n][r] = s[n][r] == kNegInf ? (kDeltaFirst ? 0.f : dl) : dp[n][r];
+                mask_tile<true, true>(s[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane, &dp[n], kDeltaFirst ? 0.f : dl);
             }
         }
 #pragma unroll
@@ -560,12 +557,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
                             s[n][r] = at[0] == kNegInf ? kNegInf : (s[n][r] - at[0]) + at[BQ];
                         }
                     }
-                    mask_tile<false>(s[n], keys, left - 32 * n, a.causal, d0 - 32 * n, lane);
-                    if constexpr (!kStartLate<T>) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)  // whatever dP is where nothing is seen
-                            dp[n][r] = s[n][r] == kNegInf ? 0.f : dp[n][r];
-                    }
+                    mask_tile<false, !kStartLate<T>>(s[n], keys, left - 32 * n, a.causal, d0 - 32 * n, lane, &dp[n]);
                 }
             }
 #pragma unroll
@@ -577,7 +569,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
                     s[n][r] = __builtin_amdgcn_exp2f(fmaf(a.c2, e, constant));
                     dp[n][r] = s[n][r] * (kStartLate<T> ? dp[n][r] + at[BQ] : dp[n][r]);  // dS
                 }
-            if (kStartLate<T> && !inner && a.causal) {  // the same, with its late delta
+            if (kStartLate<T> && !inner && a.causal) {  // as mask_tile() does where delta is there already
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
