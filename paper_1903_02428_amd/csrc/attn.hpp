@@ -2,8 +2,8 @@
 // position, masks and the scores of a 32 x 32 tile.
 //
 // The scores are a_ij = c q_i . k_j + T[bucket(j - i'), h], with i' = i + nk - nq.
-// They are held as s = a / c: the bias over c is what a tile's accumulators
-// start from, so that the matrix cores add it and far from the diagonal, where
+// They are held as s = a / c: the bias over c is what a bf16 tile's accumulators
+// start from, so that the matrix cores add it (fp32 tiles add it last), and far from the diagonal, where
 // one bucket holds all offsets, it costs nothing. p = exp(a - max) is then
 // exp2(c2 (s - m)), c2 = c log2(e).
 #pragma once
@@ -108,6 +108,23 @@ __device__ __forceinline__ f32x16 bias_tile(const float *bias, int reach, int d0
         c[r] = bias[o];
     }
     return c;
+}
+
+// The same added to scores that are there already (fp32: products begun from a bias would round every partial sum at
+// its magnitude; bf16 ones take an eighth of the additions and have 16 bits less to lose).
+template <typename T>
+constexpr bool kBiasLate = sizeof(T) == 4;
+template <bool KEYS_IN_ROWS>
+__device__ __forceinline__ void add_bias(f32x16 &c, const float *bias, int reach, int d0, int lane) {
+    lane = opaque(lane);
+    const int m = lane & 31, h = lane >> 5, base = d0 + reach + (KEYS_IN_ROWS ? 4 * h - m : m - 4 * h);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int row = 8 * (r >> 2) + (r & 3);
+        int o = KEYS_IN_ROWS ? base + row : base - row;
+        o = o < 0 ? 0 : o > 2 * reach ? 2 * reach : o;
+        c[r] += bias[o];
+    }
 }
 
 // -infinity where there is no such key (rows from `keys` on) or it comes later

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         f32x16 st[NK];
 #pragma unroll
         for (int n = 0; n < NK; ++n) st[n] = f32x16(0.f);
-        if (!inner) {
+        if (!kBiasLate<T> && !inner) {
 #pragma unroll
             for (int n = 0; n < NK; ++n) st[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
         }
@@ -127,7 +127,10 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
             }
         if (!inner) {
 #pragma unroll
-            for (int n = 0; n < NK; ++n) mask_tile<true>(st[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+            for (int n = 0; n < NK; ++n) {
+                if constexpr (kBiasLate<T>) add_bias<true>(st[n], bias, a.reach, d0 + 32 * n, lane);
+                mask_tile<true>(st[n], left - 32 * n, 32, a.causal, d0 + 32 * n, lane);
+            }
         }
         float t = kNegInf;
 #pragma unroll

@@ -25,7 +25,7 @@ constexpr int kTileOfFour = DP * sizeof(T) <= 128 ? 64 : 32;
 // partial sum at start's magnitude (a table's gradient 1.3e-6 off instead of 4e-7), so it is added after the
 // products. Where the bias holds lowest values (wild) s - top comes first and rest = -log2 sum / c2 after it.
 template <typename T>
-constexpr bool kStartLate = sizeof(T) == 4;
+constexpr bool kStartLate = kBiasLate<T>;
 struct RowStat {
     float top, start, rest;
 };
@@ -242,7 +242,6 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     st = settled(st);
     constexpr bool kDeltaFirst = DP < 128 && !kStartLate<T>;  // dP starts from it, but where registers are short
     const f32x16 no_delta(-dl);
-    const float late = kStartLate<T> && !wild ? fminf(a.c2 * st.start, kHuge) : 0.f;
 
     registers_loaded();
     f32x16 acc[DP / 32];
@@ -259,15 +258,21 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         // inner tiles: no mask, no end, one bias; they jump over what the others need
         const bool inner = left >= BK && !wild && flat(d0 - 31, d0 + BK - 1, a.reach, a.causal);
         f32x16 s[NK], dp[NK];
+        float late = 0.f;  // what fp32 scores get after the products
         if (inner) {
-            const float begin = bias[d0 > 0 ? 2 * a.reach : 0] + (kStartLate<T> ? 0.f : st.start);
+            const float begin = bias[d0 > 0 ? 2 * a.reach : 0] + st.start;
+            if (kStartLate<T>) late = fminf(a.c2 * begin, kHuge);
 #pragma unroll
-            for (int n = 0; n < NK; ++n) s[n] = f32x16(begin);
+            for (int n = 0; n < NK; ++n) s[n] = f32x16(kStartLate<T> ? 0.f : begin);
+        } else if constexpr (kStartLate<T>) {
+            late = wild ? 0.f : fminf(a.c2 * st.start, kHuge);
+#pragma unroll
+            for (int n = 0; n < NK; ++n) s[n] = f32x16(0.f);
         } else {
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
                 s[n] = bias_tile<true>(bias, a.reach, d0 + 32 * n, lane);
-                if (!wild && !kStartLate<T>) s[n] += st.start;
+                if (!wild) s[n] += st.start;
             }
         }
 #pragma unroll
@@ -281,6 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
         if (!inner) {
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
+                if constexpr (kStartLate<T>) add_bias<true>(s[n], bias, a.reach, d0 + 32 * n, lane);
                 if (wild) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[n][r] = st.top == kNegInf ? kNegInf : (s[n][r] - st.top) + st.rest;
@@ -532,7 +538,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[n][4 * q + i] = x[i], dp[n][4 * q + i] = y[i];
                 }
-            if (!inner) {
+            if (!inner && !kStartLate<T>) {
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
                     const f32x16 b = bias_tile<false>(bias, a.reach, d0 - 32 * n, lane);
@@ -550,6 +556,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             if (!inner) {
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
+                    if constexpr (kStartLate<T>) add_bias<false>(s[n], bias, a.reach, d0 - 32 * n, lane);
                     if (wild) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {

@@ -250,9 +250,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
         const bool is_far = j + F::KEYS - 1 - (r0 / a.G + nk - nq) <= -a.reach;
 #pragma unroll
         for (int u = 0; u < F::SUB; ++u) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                s[u][r] = !biased ? 0.f : is_far ? far : bias_of<T>(a, head, j + 16 * u + 4 * g + r - shift);
+            s[u] = f32x4(0.f);
 #pragma unroll
             for (int i = 0; i < F::STEPS; ++i) {
                 Piece<T> x, y;
@@ -268,6 +266,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(const Args a, int64_t
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int64_t key = j + 16 * u + 4 * g + r;
+                s[u][r] += !biased ? 0.f : is_far ? far : bias_of<T>(a, head, key - shift);
                 if (key >= end || (a.causal && key > shift)) s[u][r] = kNegInf;
             }
         }

@@ -284,3 +284,18 @@ def test_what_a_row_does_not_see_may_be_anything(pyg, i, dtype):  # noqa: F811
     nan = [torch.full_like(t, math.nan) for t in (q, k, v, grad)]
     got = call(*nan)
     assert odd(got["out"][M.any(1)]) and odd(got["grad_q"][M.any(1)]) and odd(got["grad_k"][M.any(0)]) and odd(got["grad_v"][M.any(0)])
+
+
+@pytest.mark.parametrize("qn,kn,causal", [([2], [700], False), ([3, 33], [1100, 3000], True), ([40, 90], [90, 60], False), ([300], [310], True),
+                                          ([1060], None, False)])
+@pytest.mark.parametrize("low", [-1e5, 3e4])
+def test_biases_far_larger_than_the_products(pyg, qn, kn, causal, low):  # noqa: F811
+    """fp32 products are summed by themselves and the bias added once: a bias that all keys share costs one
+    rounding at its magnitude and not one of every partial sum of 128 features (the reference's bound
+    allows four)."""
+    same = kn is None
+    kn = qn if same else kn
+    q, k, v, grad, table, lut = inputs(500, qn, kn, 2, 1, 128, torch.float32, 4, 12, causal, pyg)
+    table[:] = low
+    got = run(pyg, q, k, v, grad, table, lut, qn, kn, causal, same=same)
+    close(got, attention(q, k, v, qn, kn, table, lut, causal, grad=grad), f"{low} {qn}")
