@@ -656,7 +656,7 @@ __global__ __launch_bounds__(kBlock) void k_join_q(const float *__restrict__ par
 }
 // Key ranges of dQ, where few queries over long histories leave the card idle: 1,024
 // lone wavefronts, ranges of 256 keys or more (one query of 8 heads of 64 over 100,000 keys, bf16: all
-// gradients 4,120 us without, 274 with).
+// gradients 4,120 us without, 280 with).
 int q_splits(const Args &a) {
     const int64_t tiles = (a.Nq / 32 + a.B) * a.H;
     if (a.B < 1 || tiles >= 512 || a.Nk < 1024 * a.B || a.Nq * 4 > a.Nk) return 1;
