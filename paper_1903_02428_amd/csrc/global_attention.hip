@@ -204,8 +204,8 @@ __global__ __launch_bounds__(64 * WAVES, (kForwardWaves<T, DP, WAVES>)) void k_f
         if (a.rest) store_rows<T, DP, true>(static_cast<T *>(a.rest), row, there, a.H, head, a.D, a.vec_o, acc, mul, lane);
     if (a.stat && there && h == 0)
         *reinterpret_cast<float2 *>(a.stat + (row * a.H + head) * 2) = make_float2(top, top == kNegInf ? 0.f : __log2f(sum));
-    const bool odd = column_odd(acc);
-    if (a.causal && __any(odd)) repair<T, DP, WAVES>(nslots, top, mul, odd);
+    const bool odd = a.causal && column_odd(acc);
+    if (__any(odd)) repair<T, DP, WAVES>(nslots, top, mul, odd);
 }
 
 template <typename T, int DP, int WAVES, int BK>

@@ -348,8 +348,8 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_q(cons
     if (b.grad_q) {
         if (splits > 1) store_rows<float, DP>(dq_part, row, there, a.H, head, a.D, a.D % 4 == 0, acc, a.scale, lane);
         else store_rows<T, DP>(static_cast<T *>(b.grad_q), row, there, a.H, head, a.D, a.vec_o, acc, a.scale, lane);
-        const bool odd = column_odd(acc);
-        if (a.causal && __any(odd)) repair_q<T, DP, WAVES>(nslots, splits, dq_part, odd);
+        const bool odd = a.causal && column_odd(acc);
+        if (__any(odd)) repair_q<T, DP, WAVES>(nslots, splits, dq_part, odd);
     }
     if (mine) {
         below = wave_sum(below), above = wave_sum(above);
@@ -612,7 +612,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
             step(lds + 2 * kTile, lds + 3 * kTile, stats + 4 * BQ, i0 + BQ);
         }
     }
-    const bool odd = column_odd(dk) || column_odd(dv);
+    const bool odd = a.causal && (column_odd(dk) || column_odd(dv));
     if (splits > 1) {
         store_rows<float, DP>(dk_part, row, there, a.Hkv, hk, a.D, a.D % 4 == 0, dk, a.scale, lane);
         store_rows<float, DP>(dv_part, row, there, a.Hkv, hk, a.D, a.D % 4 == 0, dv, 1.f, lane);
@@ -620,7 +620,7 @@ __global__ __launch_bounds__(64 * WAVES, (kGradWaves<T, DP>)) void k_grad_kv(con
         store_rows<T, DP>(static_cast<T *>(b.grad_k), row, there, a.Hkv, hk, a.D, a.vec_o, dk, a.scale, lane);
         store_rows<T, DP>(static_cast<T *>(b.grad_v), row, there, a.Hkv, hk, a.D, a.vec_o, dv, 1.f, lane);
     }
-    if (a.causal && __any(odd)) repair_kv<T, DP, WAVES>(delta, splits, dk_part, odd);
+    if (__any(odd)) repair_kv<T, DP, WAVES>(delta, splits, dk_part, odd);
 }
 
 // dK and dV from the shares of the head groups [splits][2][Nk, Hkv, D], in order.
