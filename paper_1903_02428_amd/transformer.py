@@ -172,8 +172,8 @@ def global_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: tor
     q [Nq, H, D], k and v [Nk, Hkv, D] (float32 or bfloat16, D <= 128, Hkv divides H; rows and
     heads may be strided views); ptr int64 [graphs + 1], the rows of each graph's queries,
     and k_ptr those of its keys (default: the same); table [buckets, H] and buckets as
-    relative_buckets() makes it; causal: keys later than the query are not seen (the last
-    query is aligned with the last key); scale defaults to D ** -0.5. `stat` (float32
+    relative_buckets() makes it; causal: keys later than the query are not seen, whatever
+    they hold (the last query is aligned with the last key); scale defaults to D ** -0.5. `stat` (float32
     [Nq, H, 2]) receives what global_attention_backward needs, `rest` (bfloat16, out's shape)
     what rounding took from out. Rows that belong to no graph
     get zeros, but are left as they were in an `out` that the caller brings."""
